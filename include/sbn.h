@@ -468,6 +468,156 @@ int sbn_chain_check(const sbn_chain_t* c);
 
 void sbn_chain_free(sbn_chain_t* c);
 
+/* ------------------------------------------------------------------ blocks and scoring heads of language models */
+
+/*
+ * Layers over rows (tokens, or pixels) in low precision, the norm in front of
+ * them and the log probabilities behind the logits:
+ *
+ *   sbn_add_rmsnorm -> (codes, scales) -> sbn_linear_mx -> logits -> sbn_log_probs
+ *
+ * Conventions of these calls, where they differ from the ones above:
+ *   - x[rows][cols] of a type SBN_F32, SBN_BF16 or SBN_F16, columns contiguous,
+ *     rows `ld*` ELEMENTS apart (at least cols).  Pointers need the alignment of
+ *     their type only (2 or 4 bytes); codes need 16 bytes.
+ *   - rows may be 0 (nothing is launched, pointers may then be NULL); cols is at
+ *     least 1.  Extents and strides are 64-bit.
+ *   - Outputs must not overlap inputs unless a call says so.
+ *   - Run calls launch on the stream given, never allocate, never synchronise.
+ *     Sums are held in 32 bits and their order is fixed: the same call gives the
+ *     same bits.
+ */
+#define SBN_F32  0
+#define SBN_BF16 1
+#define SBN_F16  2
+
+/*
+ * Formats that hold rows in 4 or 8 bits; a row's codes are padded with zeros to
+ * whole blocks of 32 columns, B = ceil(cols / 32).
+ *   SBN_MXFP4    codes [rows][B * 16]: E2M1, two to a byte, the even column low;
+ *                scales uint8 [rows][B]: E8M0, 2^(byte - 127)
+ *   SBN_MXFP8    codes [rows][B * 32]: E4M3 (no infinities); scales as above
+ *   SBN_FP8_ROW  codes [rows][B * 32]: E4M3; scales float [rows]
+ * What codes stand for: value = element * scale.
+ *
+ * Blocks (microscaling, OCP MX v1.0): a = the largest magnitude of the block,
+ * exponent floor(log2 a) - 2 (E2M1) or - 8 (E4M3), at least -127; elements are
+ * x / 2^exponent to the nearest, ties to even, saturated at 6 or 448.  A block of
+ * zeros has byte 0.  A block that holds NaN or an infinity has byte 255 and stands
+ * for NaN.
+ * Rows: scale = a / 448, elements E4M3(x * (448 * (1 / a))), each step rounded to
+ * 32 bits, likewise.  A row whose a is below 2^-117 has scale 0; a row with NaN or
+ * an infinity has scale NaN.
+ */
+#define SBN_MXFP4   4
+#define SBN_MXFP8   5
+#define SBN_FP8_ROW 6
+
+/* Bytes of codes and of scales for rows x cols. */
+int sbn_quantized_bytes(int format, int64_t rows, int64_t cols, size_t* code_bytes_out, size_t* scale_bytes_out);
+
+int sbn_quantize(const void* x, int x_type, int64_t rows, int64_t cols, int64_t ldx, int format, void* codes,
+                 void* scales, void* stream);
+/* y = the values that the codes stand for, rounded once to y's type. */
+int sbn_dequantize(const void* codes, const void* scales, int format, int64_t rows, int64_t cols, void* y, int y_type,
+                   int64_t ldy, void* stream);
+
+/*
+ * h = x + residual (32 bits); total = h rounded to the residual's type;
+ * y = h / sqrt(mean over the columns of h^2 + eps) * weight, computed from the
+ * unrounded h; then y in 16 or 32 bits, in codes and scales, or both.
+ *   residual   NULL: h = x, and total must be NULL.  Its type r_type is x_type or
+ *              SBN_F32.
+ *   total      NULL: not written.  May be the residual itself (same ld), or x where
+ *              the types and ld agree.
+ *   weight     float [cols]; NULL: ones.
+ *   y          of x_type; NULL: not written.
+ *   format     0: no codes.  Otherwise y is taken through the format above (from
+ *              its 32-bit values).
+ * A row of zeros gives zeros.  A NaN or an infinity in a row makes the row NaN (or,
+ * for an infinity, zeros beside the NaN).  Squares are summed in 32 bits: rows with
+ * values past 1e19 / sqrt(cols) overflow to zeros.
+ */
+typedef struct {
+    int64_t rows, cols;
+    const void* x;        int x_type;  int64_t ldx;
+    const void* residual; int r_type;  int64_t ldr;
+    void* total;                       int64_t ldt;
+    const float* weight;  float eps;
+    void* y;                           int64_t ldy;
+    int format;           void* codes; void* scales;
+} sbn_rmsnorm_t;
+int sbn_add_rmsnorm(const sbn_rmsnorm_t* a, void* stream);
+
+/*
+ * A pointwise layer whose weights are held in SBN_MXFP4 (blocks of 32 input
+ * channels), laid out for the device once.
+ *
+ * sbn_mx_pack: from the library's layer description (kind SBN_CONV1X1): mask,
+ * orders, bias and activation mean what they mean for sbn_pack; removed weights
+ * become zeros, the rest is quantised by the rule above (weights with NaN or
+ * infinity: SBN_EINVAL).  go and gi are read only with a mask.  c_in need not be
+ * a multiple of 32.
+ * sbn_mx_pack_codes: from codes [c_out][B * 16] and scales [c_out][B] as
+ * sbn_quantize gives them or a checkpoint holds them; bias float [c_out] or NULL.
+ * The three are host memory or memory of `device`; work that still writes them is
+ * waited for.  Scale bytes are at most 252 (2^125); larger ones are taken as NaN.
+ * Codes past c_in in a row's last block are ignored.
+ * device = -1 keeps a host copy only (then the three are host memory).
+ * Both calls synchronise the device.
+ *
+ * sbn_mx_unpack: codes, scales, bias back to host memory (any may be NULL).
+ */
+typedef struct sbn_mx sbn_mx_t;
+int sbn_mx_pack(const sbn_layer_desc_t* layer, int device, sbn_mx_t** out);
+int sbn_mx_pack_codes(const void* codes, const void* scales, int c_in, int c_out, const float* bias, int act, int device,
+                      sbn_mx_t** out);
+int sbn_mx_unpack(const sbn_mx_t* p, void* codes, void* scales, float* bias);
+int sbn_mx_info(const sbn_mx_t* p, int* c_in, int* c_out, int* act, int* device, size_t* device_bytes);
+void sbn_mx_free(sbn_mx_t* p);
+
+/*
+ * y[r][n] = act(sum over k of X[r][k] W[n][k] + bias[n]), X and W the values that
+ * the codes stand for, summed in 32 bits and rounded once to y's type.
+ * codes / scales: [rows][c_in] in `format`.  workspace: device memory of at least
+ * sbn_linear_mx_workspace bytes (16-byte aligned; NULL where that is 0), free for
+ * other use once the launch has run; calls that overlap need one each.
+ */
+int sbn_linear_mx_workspace(const sbn_mx_t* p, int format, int64_t rows, size_t* bytes_out);
+int sbn_linear_mx(const sbn_mx_t* p, const void* codes, const void* scales, int format, int64_t rows, void* y, int y_type,
+                  int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * For every row of logits: log sum exp, the log probability of n_targets given
+ * columns, the entropy (nats) and the k likeliest columns.
+ *   lse      float [rows]
+ *   logp     float [rows][n_targets]: logits[target] - lse.  A negative target is
+ *            not scored: 0.  A target >= cols: NaN.  n_targets may be 0.
+ *   entropy  float [rows]; NULL: not written
+ *   top_ids  int64 [rows][k], top_logp float [rows][k]: by logit, descending, of
+ *            equal ones the lowest column first (-0 equals 0).  k at most SBN_MAX_TOP and cols; 0: none.
+ * Masked columns hold -infinity: log probability -infinity, no part in the entropy.
+ * A row that is masked whole: lse and every log probability -infinity, entropy 0.
+ * A row with NaN or +infinity: lse, entropy and log probabilities NaN (unscored
+ * targets still 0); top_ids then order NaN before +infinity before the rest.
+ *
+ * sbn_log_probs_backward: grad[r][i] = sum_j g_logp[r][j] [i = target j]
+ *   - p_i (G + g_entropy[r] (log p_i + entropy[r])), G = the sum of g_logp over the
+ * row's scored targets, p_i = exp(logits - lse), lse and entropy as the forward
+ * call gave them (entropy may be NULL without g_entropy; g_entropy NULL: zeros).
+ * The gradient has the logits' type and may be the logits' own memory (same ld).
+ * p_i is 0 for a masked column and in a row that is masked whole.  Targets past
+ * the columns count as not scored.
+ */
+#define SBN_MAX_TOP 64
+int sbn_log_probs_workspace(int64_t rows, int64_t cols, int k, size_t* bytes_out);
+int sbn_log_probs(const void* logits, int type, int64_t rows, int64_t cols, int64_t ld, const int64_t* targets,
+                  int n_targets, int k, float* logp, float* lse, float* entropy, int64_t* top_ids, float* top_logp,
+                  void* workspace, size_t workspace_bytes, void* stream);
+int sbn_log_probs_backward(const void* logits, int type, int64_t rows, int64_t cols, int64_t ld, const int64_t* targets,
+                           int n_targets, const float* lse, const float* entropy, const float* g_logp,
+                           const float* g_entropy, void* grad, int64_t ldg, void* stream);
+
 /* ------------------------------------------------------------------ measurement helpers */
 
 /*

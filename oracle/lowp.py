@@ -1,0 +1,118 @@
+"""Definitions in 64 bits of the low-precision rows, the norm, the product and the log probabilities (numpy).
+
+Written from the definitions alone; test infrastructure, never imported by the library."""
+import numpy as np
+
+MXFP4, MXFP8, FP8_ROW = 4, 5, 6
+E2M1 = np.array([0, 0.5, 1, 1.5, 2, 3, 4, 6])
+
+
+def _e4m3_table():
+    v = []
+    for c in range(127):
+        e, m = c >> 3, c & 7
+        v.append((8 + m) * 2.0 ** (e - 10) if e else m * 2.0 ** -9)
+    return np.array(v)
+
+
+E4M3 = _e4m3_table()
+
+
+def element_codes(v, table, sign_bit):
+    """Code of the nearest table value, ties to the even code, saturating."""
+    a = np.minimum(np.abs(v), table[-1])
+    hi = np.clip(np.searchsorted(table, a), 1, len(table) - 1)
+    lo = hi - 1
+    mid = (table[lo] + table[hi]) / 2
+    c = np.where(a < mid, lo, np.where(a > mid, hi, np.where(lo % 2 == 0, lo, hi)))
+    return (c + np.where(np.signbit(v), sign_bit, 0)).astype(np.uint8)
+
+
+def block_bytes(top, fmt):
+    """Scale byte of a block from its largest magnitude."""
+    with np.errstate(divide="ignore"):
+        _, e = np.frexp(top)
+    b = np.where(top > 0, e - 1 - (2 if fmt == MXFP4 else 8), -127)
+    return np.maximum(b, -127) + 127
+
+
+def quantize(x, fmt):
+    """Finite x [rows][cols] (float64) -> codes, scales as sbn_quantize lays them out."""
+    r, c = x.shape
+    n = -(-c // 32)
+    p = np.zeros((r, n * 32))
+    p[:, :c] = x
+    if fmt == FP8_ROW:
+        top = np.abs(x).max(1).astype(np.float32)
+        with np.errstate(divide="ignore", over="ignore", invalid="ignore"):
+            inv = np.where(top < 2.0 ** -117, np.float32(0), np.float32(448) * (np.float32(1) / top)).astype(np.float32)
+            scale = np.where(top < 2.0 ** -117, np.float32(0), top / np.float32(448)).astype(np.float32)
+        return element_codes((p.astype(np.float32) * inv[:, None]).astype(np.float64), E4M3, 128), scale
+    b = p.reshape(r, n, 32)
+    byte = block_bytes(np.abs(b).max(2), fmt)
+    v = (b / np.exp2(byte - 127.0)[:, :, None]).reshape(r, n * 32)
+    if fmt == MXFP8:
+        return element_codes(v, E4M3, 128), byte.astype(np.uint8)
+    q = element_codes(v, E2M1, 8)
+    return (q[:, 0::2] | q[:, 1::2] << 4).astype(np.uint8), byte.astype(np.uint8)
+
+
+def values(codes, scales, fmt, cols):
+    """What codes and scales stand for, float64 [rows][cols]; scale byte 255 and scale NaN are NaN."""
+    codes = np.asarray(codes)
+    if fmt == MXFP4:
+        q = np.empty((codes.shape[0], codes.shape[1] * 2), dtype=np.uint8)
+        q[:, 0::2], q[:, 1::2] = codes & 15, codes >> 4
+        v = E2M1[q & 7] * np.where(q & 8, -1.0, 1.0)
+    else:
+        v = np.append(E4M3, np.nan)[codes & 127] * np.where(codes & 128, -1.0, 1.0)
+    s = np.asarray(scales)
+    if fmt == FP8_ROW:
+        return (v * s.astype(np.float64)[:, None])[:, :cols]
+    f = np.where(s == 255, np.nan, np.exp2(s.astype(np.float64) - 127))
+    return (v.reshape(v.shape[0], -1, 32) * f[:, :, None]).reshape(v.shape)[:, :cols]
+
+
+def rmsnorm(h, weight, eps):
+    """Float64 h [rows][cols]."""
+    return h / np.sqrt(np.square(h).mean(1, keepdims=True) + eps) * (1.0 if weight is None else weight)
+
+
+def log_probs(x, targets, k):
+    """lse, logp, entropy, ids, top log probabilities of float64 logits."""
+    r, c = x.shape
+    nan = np.isnan(x).any(1) | (x == np.inf).any(1)
+    with np.errstate(all="ignore"):
+        m = x.max(1, keepdims=True)
+        e = np.where(x == -np.inf, 0.0, np.exp(x - np.where(np.isfinite(m), m, 0.0)))
+        s = e.sum(1, keepdims=True)
+        lse = np.where(s[:, 0] > 0, m[:, 0] + np.log(s[:, 0]), -np.inf)
+        lse = np.where(nan, np.nan, lse)
+        lp = np.where(nan[:, None], np.nan, np.where(x == -np.inf, -np.inf, x - lse[:, None]))
+        p = np.where(s > 0, e / s, 0.0)
+        entropy = np.where(nan, np.nan, -np.where(p > 0, p * lp, 0.0).sum(1))
+    logp = np.zeros(targets.shape)
+    for i in range(r):
+        for j, t in enumerate(targets[i]):
+            logp[i, j] = 0.0 if t < 0 else np.nan if t >= c else lp[i, t]
+    # by logit, NaN above all, descending; of equal ones (-0 equals 0) the lowest column
+    key = np.where(np.isnan(x), np.inf, x + 0.0)
+    order = np.lexsort((np.broadcast_to(np.arange(c), x.shape), -key, ~np.isnan(x)), axis=1)
+    ids = order[:, :k]
+    return lse, logp, entropy, ids, np.take_along_axis(lp, ids, 1)
+
+
+def log_probs_gradient(x, targets, g_logp, g_entropy):
+    r, c = x.shape
+    lse, _, entropy, _, _ = log_probs(x, targets, 0)
+    with np.errstate(all="ignore"):
+        lp = x - lse[:, None]
+        p = np.where((x == -np.inf) | (lse == -np.inf)[:, None], 0.0, np.exp(lp))
+        g = np.where((targets >= 0) & (targets < c), g_logp, 0.0)
+        h = 0.0 if g_entropy is None else g_entropy[:, None] * (np.where(p > 0, lp, 0.0) + entropy[:, None])
+        dx = np.where(p == 0, 0.0, -p * (g.sum(1, keepdims=True) + h))
+    for i in range(r):
+        for j, t in enumerate(targets[i]):
+            if 0 <= t < c:
+                dx[i, t] += g[i, j]
+    return dx

@@ -89,6 +89,16 @@ class ChainItem(C.Structure):
                 ("dw_pattern", C.c_void_p), ("dw_go", C.c_int)]
 
 
+class RmsNorm(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("cols", C.c_int64),
+                ("x", C.c_void_p), ("x_type", C.c_int), ("ldx", C.c_int64),
+                ("residual", C.c_void_p), ("r_type", C.c_int), ("ldr", C.c_int64),
+                ("total", C.c_void_p), ("ldt", C.c_int64),
+                ("weight", C.c_void_p), ("eps", C.c_float),
+                ("y", C.c_void_p), ("ldy", C.c_int64),
+                ("format", C.c_int), ("codes", C.c_void_p), ("scales", C.c_void_p)]
+
+
 # name -> (restype, argtypes): every symbol include/sbn.h declares
 SYMBOLS = {
     "sbn_last_error": (C.c_char_p, []),
@@ -129,6 +139,23 @@ SYMBOLS = {
     "sbn_chain_set_multi_layer": (C.c_int, [C.c_void_p, C.c_int]),
     "sbn_chain_check": (C.c_int, [C.c_void_p]),
     "sbn_chain_free": (None, [C.c_void_p]),
+    "sbn_quantized_bytes": (C.c_int, [C.c_int, C.c_int64, C.c_int64, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
+    "sbn_quantize": (C.c_int, [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_int, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "sbn_dequantize": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_void_p, C.c_int, C.c_int64, C.c_void_p]),
+    "sbn_add_rmsnorm": (C.c_int, [C.POINTER(RmsNorm), C.c_void_p]),
+    "sbn_mx_pack": (C.c_int, [C.POINTER(LayerDesc), C.c_int, C.POINTER(C.c_void_p)]),
+    "sbn_mx_pack_codes": (C.c_int, [C.c_void_p, C.c_void_p, C.c_int, C.c_int, C.c_void_p, C.c_int, C.c_int, C.POINTER(C.c_void_p)]),
+    "sbn_mx_unpack": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "sbn_mx_info": (C.c_int, [C.c_void_p] + [C.POINTER(C.c_int)] * 4 + [C.POINTER(C.c_size_t)]),
+    "sbn_mx_free": (None, [C.c_void_p]),
+    "sbn_linear_mx_workspace": (C.c_int, [C.c_void_p, C.c_int, C.c_int64, C.POINTER(C.c_size_t)]),
+    "sbn_linear_mx": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_int64, C.c_void_p, C.c_int, C.c_int64,
+                                C.c_void_p, C.c_size_t, C.c_void_p]),
+    "sbn_log_probs_workspace": (C.c_int, [C.c_int64, C.c_int64, C.c_int, C.POINTER(C.c_size_t)]),
+    "sbn_log_probs": (C.c_int, [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_int, C.c_int] +
+                               [C.c_void_p] * 6 + [C.c_size_t, C.c_void_p]),
+    "sbn_log_probs_backward": (C.c_int, [C.c_void_p, C.c_int, C.c_int64, C.c_int64, C.c_int64, C.c_void_p, C.c_int] +
+                                        [C.c_void_p] * 5 + [C.c_int64, C.c_void_p]),
     "sbn_packed_work": (C.c_int, [C.c_void_p, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t)]),
     "sbn_packed_layout": (C.c_int, [C.c_void_p, C.POINTER(C.c_size_t), C.POINTER(C.c_size_t), C.POINTER(C.c_int)]),
     "sbn_copy_bytes": (C.c_int, [C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]),

@@ -20,6 +20,10 @@ __all__ = [
     "SBN_DW_PATTERN_DENSE", "sbn_dw_pattern_groups", "sbn_dw_pattern_select", "sbn_dw_pattern_apply",
     "sbn_force_kernel_form", "sbn_chain_set_fusion", "sbn_chain_set_multi_layer", "sbn_chain_check", "SBN_K3_PATTERNS", "SBN_K3_PATTERN_DENSE", "sbn_conv3x3_pattern_taps", "sbn_conv3x3_pattern_select",
     "sbn_conv3x3_pattern_apply",
+    "SBN_F32", "SBN_BF16", "SBN_F16", "SBN_MXFP4", "SBN_MXFP8", "SBN_FP8_ROW", "SBN_MAX_TOP", "MxPacked",
+    "sbn_quantized_bytes", "sbn_quantized_empty", "sbn_quantize", "sbn_dequantize", "sbn_add_rmsnorm",
+    "sbn_mx_pack", "sbn_mx_pack_codes", "sbn_mx_unpack", "sbn_mx_info", "sbn_mx_free", "sbn_linear_mx_workspace", "sbn_linear_mx",
+    "sbn_log_probs_workspace", "sbn_log_probs", "sbn_log_probs_backward",
 ]
 
 SBN_CONV1X1, SBN_CONV3X3 = 1, 3
@@ -577,3 +581,236 @@ def sbn_roof_lds(iters: int, sink, stream=None) -> float:
 
 def sbn_roof_read(src, nbytes: int, sink, stream=None) -> None:
     _check(_lib.lib().sbn_roof_read(src.data_ptr(), nbytes, sink.data_ptr(), _stream(stream)))
+
+
+# ---- blocks and scoring heads of language models -------------------------------------------------
+
+SBN_F32, SBN_BF16, SBN_F16 = 0, 1, 2
+SBN_MXFP4, SBN_MXFP8, SBN_FP8_ROW = 4, 5, 6
+SBN_MAX_TOP = 64
+_TYPES = {}
+
+
+class MxPacked:
+    """Owner of an sbn_mx_t*; freed on garbage collection or by sbn_mx_free."""
+
+    def __init__(self, handle: int, c_in: int, c_out: int, device: int):
+        self.handle, self.c_in, self.c_out, self.device = handle, c_in, c_out, device
+
+    def __del__(self):
+        try:
+            sbn_mx_free(self)
+        except Exception:
+            pass
+
+
+def _type_of(t, what: str) -> int:
+    if not _TYPES:
+        import torch
+        _TYPES.update({torch.float32: SBN_F32, torch.bfloat16: SBN_BF16, torch.float16: SBN_F16})
+    code = _TYPES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{what} must be float32, bfloat16 or float16, not {t.dtype}")
+    return code
+
+
+def _matrix(t, what: str, rows: Optional[int] = None, cols: Optional[int] = None):
+    """(address, type, rows, cols, row stride) of a 2-D GPU tensor whose columns are contiguous."""
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{what} must be a 2-D tensor on a GPU")
+    r, c = t.shape
+    if (rows is not None and r != rows) or (cols is not None and c != cols):
+        raise ValueError(f"{what} is {r} x {c}, expected {rows} x {cols}")
+    s0, s1 = t.stride()
+    if c > 1 and s1 != 1:
+        raise ValueError(f"the columns of {what} must be contiguous")
+    if r > 1 and s0 < c:
+        raise ValueError(f"the rows of {what} overlap")
+    return t.data_ptr(), _type_of(t, what), r, c, max(s0, c) if r > 1 else c
+
+
+def _flat(t, dtype, shape, what: str, optional: bool = False):
+    """Address of a contiguous GPU tensor of the given type and shape."""
+    if t is None:
+        if optional:
+            return None
+        raise ValueError(f"{what} is missing")
+    if not t.is_cuda or t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous {dtype} tensor of shape {tuple(shape)} on a GPU")
+    return t.data_ptr()
+
+
+def _code_shapes(fmt: int, rows: int, cols: int):
+    blocks = (cols + 31) // 32
+    if fmt not in (SBN_MXFP4, SBN_MXFP8, SBN_FP8_ROW):
+        raise ValueError(f"unknown format {fmt}")
+    return (rows, blocks * (16 if fmt == SBN_MXFP4 else 32)), (rows,) if fmt == SBN_FP8_ROW else (rows, blocks)
+
+
+def _codes(codes, scales, fmt: int, rows: int, cols: int):
+    import torch
+    a, b = _code_shapes(fmt, rows, cols)
+    return _flat(codes, torch.uint8, a, "codes"), _flat(scales, torch.float32 if fmt == SBN_FP8_ROW else torch.uint8, b, "scales")
+
+
+def _bytes_of(workspace, what: str = "workspace"):
+    if workspace is None:
+        return None, 0
+    if not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError(f"{what} must be contiguous memory on a GPU")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def sbn_quantized_bytes(fmt: int, rows: int, cols: int):
+    """(bytes of codes, bytes of scales) for rows x cols."""
+    a, b = C.c_size_t(), C.c_size_t()
+    _check(_lib.lib().sbn_quantized_bytes(fmt, rows, cols, C.byref(a), C.byref(b)))
+    return a.value, b.value
+
+
+def sbn_quantized_empty(fmt: int, rows: int, cols: int, device="cuda"):
+    """Uninitialised (codes, scales) tensors for rows x cols."""
+    import torch
+    a, b = _code_shapes(fmt, rows, cols)
+    return (torch.empty(a, dtype=torch.uint8, device=device),
+            torch.empty(b, dtype=torch.float32 if fmt == SBN_FP8_ROW else torch.uint8, device=device))
+
+
+def sbn_quantize(x, fmt: int, codes, scales, stream=None) -> None:
+    xp, xt, rows, cols, ld = _matrix(x, "x")
+    cp, sp = _codes(codes, scales, fmt, rows, cols)
+    _check(_lib.lib().sbn_quantize(xp, xt, rows, cols, ld, fmt, cp, sp, _stream(stream)))
+
+
+def sbn_dequantize(codes, scales, fmt: int, y, stream=None) -> None:
+    yp, yt, rows, cols, ld = _matrix(y, "y")
+    cp, sp = _codes(codes, scales, fmt, rows, cols)
+    _check(_lib.lib().sbn_dequantize(cp, sp, fmt, rows, cols, yp, yt, ld, _stream(stream)))
+
+
+def sbn_add_rmsnorm(x, weight, eps: float, residual=None, total=None, y=None, fmt: int = 0, codes=None, scales=None, stream=None) -> None:
+    import torch
+    a = _lib.RmsNorm()
+    a.x, a.x_type, a.rows, a.cols, a.ldx = _matrix(x, "x")
+    shape = (a.rows, a.cols)
+    if residual is not None:
+        a.residual, a.r_type, _, _, a.ldr = _matrix(residual, "residual", *shape)
+    if total is not None:
+        a.total, t, _, _, a.ldt = _matrix(total, "total", *shape)
+        if residual is not None and t != a.r_type:
+            raise ValueError("total must have the residual's type")
+    if y is not None:
+        a.y, t, _, _, a.ldy = _matrix(y, "y", *shape)
+        if t != a.x_type:
+            raise ValueError("y must have x's type")
+    a.weight = _flat(weight, torch.float32, (a.cols,), "weight", optional=True)
+    a.eps = eps
+    if fmt:
+        a.format = fmt
+        a.codes, a.scales = _codes(codes, scales, fmt, *shape)
+    _check(_lib.lib().sbn_add_rmsnorm(C.byref(a), _stream(stream)))
+
+
+def sbn_mx_pack(w, go: int = 4, gi: int = 4, mask=None, bias=None, perm_out=None, perm_in=None, act: int = SBN_ACT_NONE, device: int = 0) -> MxPacked:
+    """w [c_out][1][1][c_in] (or [c_out][c_in]) on the host -> a layer whose weights are held in SBN_MXFP4."""
+    w = _f32(w)
+    if w.ndim == 2:
+        w = w[:, None, None, :]
+    d, keep = _desc(SBN_CONV1X1, w, go, gi, mask, bias, perm_out, perm_in, 1, None, act)
+    out = C.c_void_p()
+    _check(_lib.lib().sbn_mx_pack(C.byref(d), device, C.byref(out)))
+    del keep
+    return MxPacked(out.value, d.c_in, d.c_out, device)
+
+
+def sbn_mx_pack_codes(codes, scales, c_in: int, bias=None, act: int = SBN_ACT_NONE, device: int = 0) -> MxPacked:
+    """codes [c_out][blocks * 16], scales [c_out][blocks] (uint8) and bias [c_out] (float32): tensors or arrays, on the host or on the device."""
+    import torch
+
+    def take(a, dtype, what):
+        a = torch.as_tensor(a)
+        if a.dtype != dtype or (a.is_cuda and (device < 0 or a.device.index != device)):
+            raise ValueError(f"{what} must be {dtype} on the host or on device {device}")
+        return a.contiguous()
+
+    codes, scales = take(codes, torch.uint8, "codes"), take(scales, torch.uint8, "scales")
+    c_out = codes.shape[0]
+    a, b = _code_shapes(SBN_MXFP4, c_out, c_in)
+    if tuple(codes.shape) != a or tuple(scales.shape) != b:
+        raise ValueError(f"codes and scales must have shapes {a} and {b}, not {tuple(codes.shape)} and {tuple(scales.shape)}")
+    if bias is not None:
+        bias = take(bias, torch.float32, "bias")
+        if tuple(bias.shape) != (c_out,):
+            raise ValueError(f"bias must have {c_out} elements")
+    out = C.c_void_p()
+    _check(_lib.lib().sbn_mx_pack_codes(codes.data_ptr(), scales.data_ptr(), c_in, c_out, None if bias is None else bias.data_ptr(), act,
+                                        device, C.byref(out)))
+    return MxPacked(out.value, c_in, c_out, device)
+
+
+def sbn_mx_unpack(p: MxPacked):
+    """(codes, scales, bias) of a packed layer on the host."""
+    a, b = _code_shapes(SBN_MXFP4, p.c_out, p.c_in)
+    codes, scales, bias = np.empty(a, dtype=np.uint8), np.empty(b, dtype=np.uint8), np.empty(p.c_out, dtype=np.float32)
+    _check(_lib.lib().sbn_mx_unpack(p.handle, codes.ctypes.data, scales.ctypes.data, bias.ctypes.data))
+    return codes, scales, bias
+
+
+def sbn_mx_info(p: MxPacked) -> dict:
+    v, n = [C.c_int() for _ in range(4)], C.c_size_t()
+    _check(_lib.lib().sbn_mx_info(p.handle, *[C.byref(x) for x in v], C.byref(n)))
+    return dict(zip(("c_in", "c_out", "act", "device"), (x.value for x in v)), device_bytes=n.value)
+
+
+def sbn_mx_free(p: MxPacked) -> None:
+    if p is not None and p.handle:
+        _lib.lib().sbn_mx_free(p.handle)
+        p.handle = None
+
+
+def sbn_linear_mx_workspace(p: MxPacked, fmt: int, rows: int) -> int:
+    b = C.c_size_t()
+    _check(_lib.lib().sbn_linear_mx_workspace(p.handle, fmt, rows, C.byref(b)))
+    return b.value
+
+
+def sbn_linear_mx(p: MxPacked, codes, scales, fmt: int, y, workspace=None, stream=None) -> None:
+    yp, yt, rows, _, ld = _matrix(y, "y", y.shape[0], p.c_out)
+    cp, sp = _codes(codes, scales, fmt, rows, p.c_in)
+    wp, wb = _bytes_of(workspace)
+    _check(_lib.lib().sbn_linear_mx(p.handle, cp, sp, fmt, rows, yp, yt, ld, wp, wb, _stream(stream)))
+
+
+def sbn_log_probs_workspace(rows: int, cols: int, k: int) -> int:
+    b = C.c_size_t()
+    _check(_lib.lib().sbn_log_probs_workspace(rows, cols, k, C.byref(b)))
+    return b.value
+
+
+def sbn_log_probs(logits, targets, k: int, logp, lse, entropy=None, top_ids=None, top_logp=None, workspace=None, stream=None) -> None:
+    """targets int64 [rows][n] (or None); logp [rows][n], lse and entropy [rows], top_ids (int64) and top_logp [rows][k]."""
+    import torch
+    xp, xt, rows, cols, ld = _matrix(logits, "logits")
+    n = 0 if targets is None else targets.shape[-1]
+    tp = _flat(targets, torch.int64, (rows, n), "targets", optional=True)
+    lp = _flat(logp, torch.float32, (rows, n), "logp", optional=n == 0)
+    wp, wb = _bytes_of(workspace)
+    _check(_lib.lib().sbn_log_probs(xp, xt, rows, cols, ld, tp, n, k, lp, _flat(lse, torch.float32, (rows,), "lse"),
+                                    _flat(entropy, torch.float32, (rows,), "entropy", optional=True),
+                                    _flat(top_ids, torch.int64, (rows, k), "top_ids", optional=k == 0),
+                                    _flat(top_logp, torch.float32, (rows, k), "top_logp", optional=k == 0), wp, wb, _stream(stream)))
+
+
+def sbn_log_probs_backward(logits, targets, lse, entropy, g_logp, g_entropy, grad, stream=None) -> None:
+    """grad (the logits' type; may be the logits themselves) from the gradients of logp and, if not None, of the entropy."""
+    import torch
+    xp, xt, rows, cols, ld = _matrix(logits, "logits")
+    gp, gt, _, _, ldg = _matrix(grad, "grad", rows, cols)
+    if gt != xt:
+        raise ValueError("grad must have the logits' type")
+    n = 0 if targets is None else targets.shape[-1]
+    _check(_lib.lib().sbn_log_probs_backward(xp, xt, rows, cols, ld, _flat(targets, torch.int64, (rows, n), "targets", optional=True), n,
+                                             _flat(lse, torch.float32, (rows,), "lse"),
+                                             _flat(entropy, torch.float32, (rows,), "entropy", optional=g_entropy is None),
+                                             _flat(g_logp, torch.float32, (rows, n), "g_logp", optional=n == 0),
+                                             _flat(g_entropy, torch.float32, (rows,), "g_entropy", optional=True), gp, ldg, _stream(stream)))

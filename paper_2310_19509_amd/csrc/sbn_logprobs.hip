@@ -1,0 +1,502 @@
+// Log probabilities of given columns, entropy and the likeliest columns of rows of logits; the gradient.
+//
+// One pass over the logits, bound by reading them.  Every lane keeps a running maximum m, s = sum e^(x - m) and
+// t = sum e^(x - m) (x - m) of the columns it has seen; two such triples join by
+//     f = e^(m' - m):   s = s' f,   t = (t' + (m' - m) s') f
+// so that lse = m + log s and the entropy log s - t / s need no second pass.  The likeliest columns come from the same
+// pass: the k-th largest of the 64 lanes' running maxima is a value that at least k columns reach, so a wave puts
+// aside only what is larger (a few hundred columns of a long row) and chooses among those at the end.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "sbn_mx.h"
+#include "sbn_ops.h"
+
+namespace sbn {
+namespace {
+
+constexpr int kWaves = 4;                       // of a workgroup
+constexpr int kHold = 1024;                     // columns a wave can have put aside
+constexpr int kStep = 512;                      // columns of a wave's step: 64 lanes x 8
+constexpr float kLog2e = 1.44269504f;
+constexpr float kLow = -3.402823466e38f;        // in the place of -infinity as a maximum: differences stay defined
+
+struct Stat {
+    float m, s, t;
+};
+// Far below the maximum e^d is 0 in 32 bits and its product with d, -infinity where the column is masked, has to be too.
+__device__ inline float bounded(float d) { return fmaxf(d, -200.0f); }
+__device__ inline float exp_of(float d) { return __builtin_amdgcn_exp2f(d * kLog2e); }
+
+__device__ inline void raise(Stat& a, float m)
+{
+    const float d = bounded(a.m - m), f = exp_of(d);
+    a.t = __builtin_fmaf(d, a.s, a.t) * f;
+    a.s *= f;
+    a.m = m;
+}
+__device__ inline Stat join(Stat a, Stat b)
+{
+    const float m = fmaxf(a.m, b.m);
+    raise(a, m);
+    raise(b, m);
+    return {m, a.s + b.s, a.t + b.t};
+}
+__device__ inline Stat wave_join(Stat a)
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) {
+        const Stat b = {__shfl_xor(a.m, d), __shfl_xor(a.s, d), __shfl_xor(a.t, d)};
+        // (the same pair in the same order on both lanes, so that both have the same bits)
+        a = (threadIdx.x & d) ? join(b, a) : join(a, b);
+    }
+    return a;
+}
+// Adds eight columns.  NaN and +infinity make s NaN: e^(inf - inf).
+__device__ inline void add(Stat& a, const float (&v)[8])
+{
+    float top = v[0];
+#pragma unroll
+    for (int j = 1; j < 8; ++j) top = fmaxf(top, v[j]);
+    if (top > a.m) raise(a, top);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const float d = v[j] - a.m, e = exp_of(d);
+        a.s += e;
+        a.t = __builtin_fmaf(e, bounded(d), a.t);
+    }
+}
+
+// The order of the alternatives: larger logits first, of equal ones the lower column.  NaN is above +infinity, -0 equals 0.
+__device__ inline unsigned order_of(float x)
+{
+    if (x != x) return 0xFFFFFFFFu;
+    const unsigned b = __builtin_bit_cast(unsigned, x + 0.0f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ inline float logit_of(unsigned order)
+{
+    return order == 0xFFFFFFFFu ? __builtin_nanf("") : __builtin_bit_cast(float, order & 0x80000000u ? order ^ 0x80000000u : ~order);
+}
+typedef unsigned long long Key;                 // order << 32 | ~column: of two equal logits the lower column is the larger key
+__device__ inline Key key_of(float x, unsigned col) { return (Key)order_of(x) << 32 | (unsigned)~col; }
+
+// The k-th largest of the 64 lanes' values (k in 1 .. 64), the same on all lanes: bit by bit, the largest value that at least k lanes reach.
+__device__ inline unsigned kth_of_lanes(unsigned v, int k)
+{
+    unsigned r = 0;
+    for (int b = 31; b >= 0; --b) {
+        const unsigned trial = r | 1u << b;
+        if (__popcll(__ballot(v >= trial)) >= k) r = trial;
+    }
+    return r;
+}
+
+// Orders a wave's accesses to its own LDS list (the hardware keeps them in order; this keeps the compiler from moving them).
+__device__ inline void wave_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Moves the k largest of a wave's n keys (n <= kHold) to the front of its list, in any order; fewer than k are left as they are.
+// Returns their number.  All keys differ.
+__device__ inline int keep_largest(Key* list, int n, int k)
+{
+    wave_fence();
+    if (n <= k) return n;
+    const int lane = threadIdx.x & 63, rounds = (n + 63) / 64;
+    Key v[kHold / 64];
+#pragma unroll
+    for (int i = 0; i < kHold / 64; ++i) v[i] = i < rounds && i * 64 + lane < n ? list[i * 64 + lane] : 0;      // (no key is 0)
+    Key r = 0;
+    for (int b = 63; b >= 0; --b) {
+        const Key trial = r | (Key)1 << b;
+        int count = 0;
+#pragma unroll
+        for (int i = 0; i < kHold / 64; ++i)
+            if (i < rounds) count += __popcll(__ballot(v[i] >= trial));
+        if (count >= k) r = trial;
+        if (count == k) break;
+    }
+    int at = 0;
+#pragma unroll
+    for (int i = 0; i < kHold / 64; ++i)
+        if (i < rounds) {
+            const unsigned long long keep = __ballot(v[i] >= r);
+            if (v[i] >= r) list[at + __popcll(keep & ((1ull << lane) - 1))] = v[i];
+            at += __popcll(keep);
+        }
+    wave_fence();
+    return at;
+}
+
+// A wave's search for the k largest keys of the columns that it is shown in ascending order.
+struct Search {
+    Key* list;
+    int n, k;
+    float least;                                // what at least k columns seen reach; NaN: not known yet
+    __device__ void start(Key* l, int k_) { list = l, n = 0, k = k_, least = __builtin_nanf(""); }
+    // A bound from the lanes' largest values so far (NaN counts as above all, and then as no bound).
+    __device__ void bound(float lane_top)
+    {
+        const float b = logit_of(kth_of_lanes(order_of(lane_top), k));
+        if (!(least >= b)) least = b;
+    }
+    // `equal`: columns equal to the bound count (those that it was taken from); later ones lose to them.
+    __device__ void show(const float (&v)[8], unsigned col, bool equal)
+    {
+        float top = v[0];
+        bool odd = v[0] != v[0];
+#pragma unroll
+        for (int j = 1; j < 8; ++j) top = fmaxf(top, v[j]), odd |= v[j] != v[j];
+        if (!__any(odd || (equal ? !(top < least) : !(top <= least)))) return;
+        if (n > kHold - kStep) {
+            n = keep_largest(list, n, k);
+            bound_from_list();
+        }
+        const unsigned long long below = (1ull << (threadIdx.x & 63)) - 1;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool in = col + j < limit && (equal ? !(v[j] < least) : !(v[j] <= least));
+            const unsigned long long all = __ballot(in);
+            if (in) list[n + __popcll(all & below)] = key_of(v[j], col + j);
+            n += __popcll(all);
+        }
+    }
+    unsigned limit;                             // columns of the row: what lies past them is no column
+    __device__ void bound_from_list()
+    {
+        const int lane = threadIdx.x & 63;
+        const unsigned o = lane < n ? (unsigned)(list[lane] >> 32) : 0xFFFFFFFFu;
+        unsigned low = o;
+#pragma unroll
+        for (int d = 32; d; d >>= 1) low = min(low, (unsigned)__shfl_xor((int)low, d));
+        if (n >= k) {
+            const float b = logit_of(low);
+            if (!(least >= b)) least = b;
+        }
+    }
+};
+
+// What a slice of a row leaves for the join: workspace [row][slice], keys [row][slice][k].
+struct Part {
+    Stat st;
+    unsigned n;
+};
+
+struct Args {
+    long long rows, ld;
+    unsigned cols, per;                         // columns of a row, of a slice (a multiple of 8)
+    int slices, k, n_targets;
+    const int64_t* targets;
+    float *logp, *lse, *entropy, *top_logp;
+    int64_t* top_ids;
+    Part* parts;
+    Key* keys;
+};
+
+template <class T>
+__device__ inline void finish_row(const Args& a, const T* x, long long row, const Stat& st, Key* list, int n)
+{
+    const int lane = threadIdx.x & 63;
+    const bool empty = st.m == kLow && st.s == 0.0f;                      // no column above -infinity
+    const float ls = logf(st.s);
+    const float lse = empty ? -__builtin_inff() : st.m + ls;
+    auto log_prob = [&](float v) { return st.s != st.s ? st.s : v == -__builtin_inff() ? v : v - lse; };
+    if (threadIdx.x == 0) {
+        a.lse[row] = st.s != st.s ? st.s : lse;
+        if (a.entropy) a.entropy[row] = empty ? 0.0f : ls - st.t / st.s;
+    }
+    for (int j = threadIdx.x; j < a.n_targets; j += 64 * kWaves) {
+        const int64_t c = a.targets[row * a.n_targets + j];
+        float r = 0.0f;
+        if (c >= (int64_t)a.cols)
+            r = __builtin_nanf("");
+        else if (c >= 0)
+            r = log_prob(Elem<T>::get(x[c]));
+        a.logp[row * a.n_targets + j] = r;
+    }
+    if (a.k && threadIdx.x < 64) {                                        // n = k keys: every one's place is the number of larger ones
+        const Key mine = lane < n ? list[lane] : 0;
+        int place = 0;
+        for (int i = 0; i < n; ++i) place += list[i] > mine;
+        if (lane < n) {
+            a.top_ids[row * a.k + place] = (int64_t)(unsigned)~(unsigned)mine;
+            a.top_logp[row * a.k + place] = log_prob(logit_of((unsigned)(mine >> 32)));
+        }
+    }
+}
+
+// Joins the waves' lists (at most k keys each) to the first one's; all threads call it.
+__device__ inline int join_lists(Key (*lists)[kHold], int* counts, int n, int k)
+{
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    if (lane == 0) counts[wave] = n;
+    __syncthreads();
+    int at = counts[0];
+    if (wave == 0) {
+        for (int w = 1; w < kWaves; ++w) {
+            if (lane < counts[w]) lists[0][at + lane] = lists[w][lane];
+            at += counts[w];
+        }
+        at = keep_largest(lists[0], at, k);
+    }
+    return at;
+}
+
+// One slice of a row to a workgroup: its waves take steps of 512 columns in turn, so that each sees ascending columns.
+template <class T, bool TOP>
+__global__ __launch_bounds__(64 * kWaves) void score_kernel(const T* __restrict__ logits, const Args a)
+{
+    __shared__ Key lists[TOP ? kWaves : 1][TOP ? kHold : 1];
+    __shared__ Stat stats[kWaves];
+    __shared__ int counts[kWaves];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const long long row = blockIdx.x / (unsigned)a.slices;
+    const unsigned slice = blockIdx.x % (unsigned)a.slices;
+    const T* const x = logits + row * a.ld;
+    const unsigned begin = slice * a.per, end = min(begin + a.per, a.cols);
+    constexpr int U = 4;                                                  // steps under way at once
+    constexpr unsigned kTurn = kStep * kWaves;                            // columns of one step of all waves
+
+    Stat st = {kLow, 0.0f, 0.0f};
+    Search find;
+    if constexpr (TOP) find.start(lists[wave], a.k), find.limit = end;
+    unsigned turn = 0, next_bound = 0;
+    for (unsigned c0 = begin + wave * kStep; c0 < end; c0 += U * kTurn, ++turn) {
+        Raw<T> raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = fetch_unit(x, (c0 + u * kTurn) / 8 + lane, end);
+        float v[U][8];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            expand_unit(raw[u], x, (c0 + u * kTurn) / 8 + lane, end, v[u], -__builtin_inff());
+            add(st, v[u]);
+        }
+        if constexpr (TOP) {
+            const bool bound = turn == next_bound;                        // at turns 0, 1, 3, 7, ...: the bound rises with the logarithm of what was seen
+            if (bound) next_bound = 2 * turn + 1;
+            if (bound) find.bound(st.s != st.s ? __builtin_nanf("") : st.m == kLow ? -__builtin_inff() : st.m);
+#pragma unroll
+            for (int u = 0; u < U; ++u) find.show(v[u], c0 + u * kTurn + lane * 8, bound);
+        }
+    }
+    st = wave_join(st);
+    if (lane == 0) stats[wave] = st;
+    int n = 0;
+    if constexpr (TOP) {
+        n = keep_largest(find.list, find.n, a.k);
+        n = join_lists(lists, counts, n, a.k);                            // (its barrier covers stats)
+    } else {
+        __syncthreads();
+    }
+    st = stats[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) st = join(st, stats[w]);
+    if (a.slices == 1) {
+        finish_row(a, x, row, st, lists[0], n);
+    } else {
+        if (threadIdx.x == 0) a.parts[blockIdx.x] = {st, (unsigned)n};
+        if constexpr (TOP)
+            if (threadIdx.x < n) a.keys[(long long)blockIdx.x * a.k + threadIdx.x] = lists[0][threadIdx.x];
+    }
+}
+
+// Joins the slices of a row.
+constexpr int kMaxSlices = 64;
+template <class T, bool TOP>
+__global__ __launch_bounds__(64 * kWaves) void join_kernel(const T* __restrict__ logits, const Args a)
+{
+    __shared__ Key lists[TOP ? kWaves : 1][TOP ? kHold : 1];
+    __shared__ int counts[kWaves];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const long long row = blockIdx.x;
+    const Part* const parts = a.parts + row * a.slices;
+    Part p = {{kLow, 0.0f, 0.0f}, 0};
+    if (lane < a.slices) p = parts[lane];
+    const Stat st = wave_join(p.st);                                      // (every wave: the same bits)
+    int n = 0;
+    if constexpr (TOP) {
+        // a wave takes every fourth slice: at most 16 x 64 keys
+        for (int s = wave; s < a.slices; s += kWaves) {
+            const int c = __shfl((int)p.n, s);
+            if (lane < c) lists[wave][n + lane] = a.keys[(row * a.slices + s) * a.k + lane];
+            n += c;
+        }
+        n = keep_largest(lists[wave], n, a.k);
+        n = join_lists(lists, counts, n, a.k);
+    }
+    finish_row(a, logits + row * a.ld, row, st, lists[0], n);
+}
+
+// Slices of a row: enough workgroups to fill the machine, at least 4096 columns each.
+int slices_of(long long rows, long long cols)
+{
+    constexpr long long kWorkgroups = 1024;
+    const long long by_work = cols / 4096, by_rows = rows >= kWorkgroups ? 1 : kWorkgroups / std::max(rows, 1ll);
+    return (int)std::max(1ll, std::min({by_work, by_rows, (long long)kMaxSlices}));
+}
+
+struct BackArgs {
+    long long ld, ldg;
+    unsigned cols, per;
+    int slices, n_targets;
+    const int64_t* targets;
+    const float *lse, *entropy, *g_logp, *g_entropy;
+};
+
+// dx = - p (G + g_H (log p + H)), plus g_j at target j.  Bound by reading the logits and writing the gradient; a lane holds the
+// targets of eight columns only if one of them falls there, which is looked up in LDS per unit for up to kTargets at a time.
+constexpr int kTargets = 64;
+template <class T>
+__global__ __launch_bounds__(256) void gradient_kernel(const T* logits, T* grad, const BackArgs a)
+{
+    __shared__ float lds_g[kTargets];
+    __shared__ unsigned lds_t[kTargets];
+    const long long row = blockIdx.x / (unsigned)a.slices;
+    const unsigned slice = blockIdx.x % (unsigned)a.slices;
+    const T* const x = logits + row * a.ld;
+    T* const g = grad + row * a.ldg;
+    const unsigned begin = slice * a.per, end = min(begin + a.per, a.cols);
+    const float lse = a.lse[row];
+    const float gh = a.g_entropy ? a.g_entropy[row] : 0.0f, h = a.g_entropy ? a.entropy[row] : 0.0f;
+    const int64_t* const targets = a.targets + row * a.n_targets;
+    const float* const gl = a.g_logp + row * a.n_targets;
+    float total = 0.0f;
+    for (int j = 0; j < a.n_targets; ++j) {                               // (every thread the same sum: a row's targets are few)
+        const int64_t c = targets[j];
+        if (c >= 0 && c < (int64_t)a.cols) total += gl[j];
+    }
+    const bool empty = lse == -__builtin_inff();
+    const int held = min(a.n_targets, kTargets);
+    for (int j = threadIdx.x; j < held; j += 256) {
+        const int64_t c = targets[j];
+        lds_t[j] = c >= 0 && c < (int64_t)a.cols ? (unsigned)c : 0xFFFFFFFFu;
+        lds_g[j] = gl[j];
+    }
+    __syncthreads();
+    constexpr int U = 4;
+    for (unsigned c0 = begin + threadIdx.x * 8; c0 < end; c0 += U * 2048) {
+        Raw<T> raw[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) raw[u] = fetch_unit(x, (c0 + u * 2048) / 8, end);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const unsigned c = c0 + u * 2048;
+            if (c >= end) break;
+            float v[8];
+            expand_unit(raw[u], x, c / 8, end, v, -__builtin_inff());
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float lp = v[j] - lse;
+                const float p = empty ? 0.0f : exp_of(lp);
+                v[j] = p == 0.0f ? 0.0f : -p * __builtin_fmaf(gh, lp + h, total);
+            }
+            for (int j = 0; j < held; ++j) {
+                const unsigned d = lds_t[j] - c;
+                if (d < 8) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] += d == i ? lds_g[j] : 0.0f;
+                }
+            }
+            for (int j = kTargets; j < a.n_targets; ++j) {
+                const int64_t d = targets[j] - (int64_t)c;
+                if (d >= 0 && d < 8) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[i] += d == i && targets[j] < (int64_t)a.cols ? gl[j] : 0.0f;
+                }
+            }
+            store_unit(g, c / 8, end, v);
+        }
+    }
+}
+
+constexpr long long kMostGroups = 1ll << 23;                              // workgroups of 256 threads a launch
+
+template <class T>
+int run_scores(const T* logits, Args a, hipStream_t stream)
+{
+    const long long most = std::max(1ll, kMostGroups / a.slices), all = a.rows;
+    for (long long r0 = 0; r0 < all; r0 += most) {
+        Args b = a;
+        b.rows = std::min(most, all - r0);
+        b.targets = a.targets + r0 * a.n_targets;
+        if (a.logp) b.logp = a.logp + r0 * a.n_targets;
+        b.lse = a.lse + r0;
+        if (a.entropy) b.entropy = a.entropy + r0;
+        if (a.k) b.top_ids = a.top_ids + r0 * a.k, b.top_logp = a.top_logp + r0 * a.k;
+        if (a.parts) b.parts = a.parts + r0 * a.slices;
+        if (a.keys) b.keys = a.keys + r0 * a.slices * a.k;
+        const T* const x = logits + r0 * a.ld;
+        const unsigned groups = (unsigned)(b.rows * a.slices);
+        if (a.k)
+            score_kernel<T, true><<<groups, 64 * kWaves, 0, stream>>>(x, b);
+        else
+            score_kernel<T, false><<<groups, 64 * kWaves, 0, stream>>>(x, b);
+        if (a.slices > 1) {
+            if (a.k)
+                join_kernel<T, true><<<(unsigned)b.rows, 64 * kWaves, 0, stream>>>(x, b);
+            else
+                join_kernel<T, false><<<(unsigned)b.rows, 64 * kWaves, 0, stream>>>(x, b);
+        }
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return fail(SBN_EHIP, "sbn_log_probs: %s", hipGetErrorString(e));
+    }
+    return SBN_OK;
+}
+
+unsigned per_slice(long long cols, int slices) { return (unsigned)((cols + 8ll * slices - 1) / (8ll * slices) * 8); }
+
+template <class T>
+int run_gradient(const T* logits, T* grad, long long rows, BackArgs a, hipStream_t stream)
+{
+    const long long most = std::max(1ll, kMostGroups / a.slices);
+    for (long long r0 = 0; r0 < rows; r0 += most) {
+        BackArgs b = a;
+        b.targets = a.targets + r0 * a.n_targets, b.g_logp = a.g_logp + r0 * a.n_targets, b.lse = a.lse + r0;
+        if (a.g_entropy) b.entropy = a.entropy + r0, b.g_entropy = a.g_entropy + r0;
+        gradient_kernel<T><<<(unsigned)(std::min(most, rows - r0) * a.slices), 256, 0, stream>>>(logits + r0 * a.ld, grad + r0 * a.ldg, b);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return fail(SBN_EHIP, "sbn_log_probs_backward: %s", hipGetErrorString(e));
+    }
+    return SBN_OK;
+}
+
+}  // namespace
+
+size_t log_probs_workspace(long long rows, long long cols, int k)
+{
+    const int slices = slices_of(rows, cols);
+    return slices == 1 ? 0 : (size_t)rows * slices * (sizeof(Part) + (size_t)k * sizeof(Key));
+}
+
+int launch_log_probs(const void* logits, int type, long long rows, long long cols, long long ld, const int64_t* targets, int n_targets, int k,
+                     float* logp, float* lse, float* entropy, int64_t* top_ids, float* top_logp, void* workspace, void* stream)
+{
+    Args a = {};
+    a.rows = rows, a.ld = ld, a.cols = (unsigned)cols, a.k = k, a.n_targets = n_targets, a.targets = targets;
+    a.slices = slices_of(rows, cols), a.per = per_slice(cols, a.slices);
+    a.logp = logp, a.lse = lse, a.entropy = entropy, a.top_ids = top_ids, a.top_logp = top_logp;
+    if (a.slices > 1) {
+        a.keys = (Key*)workspace;                                         // (8-byte entries first)
+        a.parts = (Part*)((char*)workspace + (size_t)rows * a.slices * k * sizeof(Key));
+    }
+    const hipStream_t s = (hipStream_t)stream;
+    return type == SBN_F32 ? run_scores((const float*)logits, a, s) : type == SBN_BF16 ? run_scores((const __bf16*)logits, a, s)
+                                                                                     : run_scores((const _Float16*)logits, a, s);
+}
+
+int launch_log_probs_backward(const void* logits, int type, long long rows, long long cols, long long ld, const int64_t* targets, int n_targets,
+                              const float* lse, const float* entropy, const float* g_logp, const float* g_entropy, void* grad, long long ldg, void* stream)
+{
+    BackArgs a = {};
+    a.ld = ld, a.ldg = ldg, a.cols = (unsigned)cols, a.n_targets = n_targets, a.targets = targets;
+    a.slices = (int)std::max(1ll, std::min({cols / 8192, rows >= 2048 ? 1ll : 2048 / rows, 4096ll})), a.per = per_slice(cols, a.slices);
+    a.lse = lse, a.entropy = entropy, a.g_logp = g_logp, a.g_entropy = g_entropy;
+    const hipStream_t s = (hipStream_t)stream;
+    return type == SBN_F32 ? run_gradient((const float*)logits, (float*)grad, rows, a, s)
+         : type == SBN_BF16 ? run_gradient((const __bf16*)logits, (__bf16*)grad, rows, a, s)
+                            : run_gradient((const _Float16*)logits, (_Float16*)grad, rows, a, s);
+}
+
+}  // namespace sbn

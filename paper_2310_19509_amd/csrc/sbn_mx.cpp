@@ -1,0 +1,467 @@
+// Entry points of the low-precision and scoring calls: argument checks, the packer of 4-bit weights, dispatch.
+#include <hip/hip_runtime_api.h>
+
+#include <cmath>
+#include <cstring>
+#include <memory>
+
+#include "sbn_mx.h"
+
+using namespace sbn;
+
+namespace {
+
+constexpr int64_t kMostCols = 0x7FFFFFFFll - 63;        // columns of a row: the kernels count them in 31 bits
+constexpr int64_t kMostRows = 1ll << 40;
+
+int type_bytes(int type) { return type == SBN_F32 ? 4 : type == SBN_BF16 || type == SBN_F16 ? 2 : 0; }
+bool is_format(int f) { return f == SBN_MXFP4 || f == SBN_MXFP8 || f == SBN_FP8_ROW; }
+bool aligned(const void* p, size_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+int check_extents(const char* who, int64_t rows, int64_t cols)
+{
+    if (rows < 0 || rows > kMostRows) return fail(SBN_EINVAL, "%s: rows out of range", who);
+    if (cols < 1 || cols > kMostCols) return fail(SBN_EINVAL, "%s: columns out of range", who);
+    return SBN_OK;
+}
+// A matrix of rows: its type, row stride and alignment.
+int check_rows(const char* who, const char* name, const void* p, int type, int64_t cols, int64_t ld)
+{
+    const int b = type_bytes(type);
+    if (!b) return fail(SBN_EINVAL, "%s: %s has unknown type %d", who, name, type);
+    if (!p) return fail(SBN_EINVAL, "%s: %s is NULL", who, name);
+    if (!aligned(p, b)) return fail(SBN_EINVAL, "%s: %s is not aligned to its type", who, name);
+    if (ld < cols || ld > (int64_t)1 << 40) return fail(SBN_EINVAL, "%s: %s has row stride %lld for %lld columns", who, name, (long long)ld, (long long)cols);
+    return SBN_OK;
+}
+int check_codes(const char* who, int format, const void* codes, const void* scales)
+{
+    if (!codes || !scales) return fail(SBN_EINVAL, "%s: codes or scales are NULL", who);
+    if (!aligned(codes, 16)) return fail(SBN_EINVAL, "%s: codes must be 16-byte aligned", who);
+    if (format == SBN_FP8_ROW && !aligned(scales, 4)) return fail(SBN_EINVAL, "%s: scales must be 4-byte aligned", who);
+    return SBN_OK;
+}
+
+// ---- the quantisation rule on the host, for packing -------------------------------------------
+
+uint8_t e2m1(float v)                                   // v already divided by the scale
+{
+    const float a = std::fabs(v);
+    const float unit = a < 2.0f ? 0.5f : a < 4.0f ? 1.0f : 2.0f;
+    const float q = std::fmin(std::nearbyint(a / unit) * unit, 6.0f);        // (ties to even multiples: even codes)
+    const uint8_t c = q < 2.0f ? (uint8_t)(q * 2.0f) : q < 4.0f ? (uint8_t)(q + 2.0f) : (uint8_t)(q / 2.0f + 4.0f);
+    return c | (std::signbit(v) ? 8 : 0);
+}
+
+void quantize_row(const float* w, int n, uint8_t* codes, uint8_t* scales)
+{
+    for (int b = 0; b * 32 < n; ++b) {
+        const int m = n - b * 32 < 32 ? n - b * 32 : 32;
+        float top = 0.0f;
+        for (int i = 0; i < m; ++i) top = std::fmax(top, std::fabs(w[b * 32 + i]));
+        uint32_t bits;
+        std::memcpy(&bits, &top, 4);
+        const int byte = (int)(bits >> 23) > 2 ? (int)(bits >> 23) - 2 : 0;
+        scales[b] = (uint8_t)byte;
+        for (int i = 0; i < 32; ++i) {
+            const uint8_t c = i < m ? e2m1(std::ldexp(w[b * 32 + i], 127 - byte)) : 0;
+            uint8_t& to = codes[b * 16 + i / 2];
+            to = (uint8_t)(i & 1 ? to | c << 4 : c);
+        }
+    }
+}
+
+// ---- the packed layer ---------------------------------------------------------------------------
+
+struct DeviceScope {                                    // the given device is current until the scope ends
+    int prev = 0;
+    hipError_t err;
+    explicit DeviceScope(int d)
+    {
+        (void)hipGetDevice(&prev);
+        err = hipSetDevice(d);
+    }
+    ~DeviceScope() { (void)hipSetDevice(prev); }
+};
+struct DeviceMemory {                                   // freed when the scope ends
+    void* p = nullptr;
+    ~DeviceMemory()
+    {
+        if (p) (void)hipFree(p);
+    }
+};
+
+void release(sbn_mx* p)
+{
+    if (!p) return;
+    if (p->d_blob) {
+        DeviceScope on(p->device);
+        (void)hipFree(p->d_blob);
+    }
+    delete p;
+}
+struct Release {
+    void operator()(sbn_mx* p) const { release(p); }
+};
+using Holder = std::unique_ptr<sbn_mx, Release>;
+
+Holder make(int c_in, int c_out, int act, bool has_bias, int device)
+{
+    Holder h(new sbn_mx);
+    h->c_in = c_in, h->c_out = c_out, h->act = act, h->has_bias = has_bias, h->device = device;
+    h->blocks = (c_in + 31) / 32;
+    h->steps = (c_in + 127) / 128;
+    h->quads = (h->steps + 3) / 4;
+    h->tile_rows = (c_out + 15) / 16;
+    return h;
+}
+
+size_t align256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+// codes, scales, bias: host memory, or memory of the device
+int upload(sbn_mx* p, const void* codes, const void* scales, const float* bias)
+{
+    int ndev = 0;
+    hipError_t e = hipGetDeviceCount(&ndev);
+    if (e != hipSuccess) return fail(SBN_EHIP, "hipGetDeviceCount: %s", hipGetErrorString(e));
+    if (p->device >= ndev) return fail(SBN_EINVAL, "device %d does not exist (%d visible)", p->device, ndev);
+    DeviceScope on(p->device);
+    if (on.err != hipSuccess) return fail(SBN_EHIP, "hipSetDevice: %s", hipGetErrorString(on.err));
+    if ((e = hipDeviceSynchronize()) != hipSuccess) return fail(SBN_EHIP, "hipDeviceSynchronize: %s", hipGetErrorString(e));
+    (void)hipDeviceGetAttribute(&p->cus, hipDeviceAttributeMultiprocessorCount, p->device);
+    const size_t b_codes = align256((size_t)p->tile_rows * p->steps * 1024), b_scales = align256((size_t)p->tile_rows * p->quads * 256);
+    const size_t b_bias = align256((size_t)p->tile_rows * 16 * sizeof(float));
+    const size_t in_codes = (size_t)p->c_out * p->blocks * 16, in_scales = (size_t)p->c_out * p->blocks;
+    auto get = [&](void** to, size_t n) {
+        e = hipMalloc(to, n);
+        return e == hipSuccess ? SBN_OK : fail(e == hipErrorOutOfMemory ? SBN_ENOMEM : SBN_EHIP, "hipMalloc(%zu): %s", n, hipGetErrorString(e));
+    };
+    if (int rc = get(&p->d_blob, b_codes + b_scales + b_bias)) return rc;
+    p->device_bytes = b_codes + b_scales + b_bias;
+    p->d_codes = (uint8_t*)p->d_blob;
+    p->d_scales = p->d_codes + b_codes;
+    p->d_bias = (float*)(p->d_scales + b_scales);
+    DeviceMemory staged;
+    if (int rc = get(&staged.p, align256(in_codes) + in_scales)) return rc;
+    uint8_t *const c = (uint8_t*)staged.p, *const s = c + align256(in_codes);
+    if ((e = hipMemcpy(c, codes, in_codes, hipMemcpyDefault)) != hipSuccess || (e = hipMemcpy(s, scales, in_scales, hipMemcpyDefault)) != hipSuccess)
+        return fail(SBN_EHIP, "hipMemcpy: %s", hipGetErrorString(e));
+    std::unique_ptr<char[]> zeros(new char[b_bias]());
+    if ((e = hipMemcpy(p->d_bias, zeros.get(), b_bias, hipMemcpyHostToDevice)) != hipSuccess ||
+        (bias && (e = hipMemcpy(p->d_bias, bias, (size_t)p->c_out * sizeof(float), hipMemcpyDefault)) != hipSuccess))
+        return fail(SBN_EHIP, "hipMemcpy: %s", hipGetErrorString(e));
+    if (int rc = launch_mx_layout(p, c, s, false, nullptr, nullptr)) return rc;
+    if ((e = hipDeviceSynchronize()) != hipSuccess) return fail(SBN_EHIP, "sbn_mx layout: %s", hipGetErrorString(e));
+    return SBN_OK;
+}
+
+int finish_pack(Holder h, const void* codes, const void* scales, const float* bias, sbn_mx_t** out)
+{
+    if (h->device < 0) {
+        const size_t n = (size_t)h->c_out * h->blocks;
+        h->codes.assign((const uint8_t*)codes, (const uint8_t*)codes + n * 16);
+        h->scales.assign((const uint8_t*)scales, (const uint8_t*)scales + n);
+        h->bias.assign(h->c_out, 0.0f);
+        if (bias) h->bias.assign(bias, bias + h->c_out);
+        if (const int tail = h->c_in % 32)                              // codes past c_in are no weights
+            for (int r = 0; r < h->c_out; ++r)
+                for (int i = tail; i < 32; ++i) h->codes[((size_t)r * h->blocks + h->blocks - 1) * 16 + i / 2] &= i & 1 ? 0x0F : 0xF0;
+        for (auto& s : h->scales) s = s > 252 ? 255 : s;
+    } else if (int rc = upload(h.get(), codes, scales, bias)) {
+        return rc;
+    }
+    *out = h.release();
+    return SBN_OK;
+}
+
+int check_layer(const char* who, int c_in, int c_out, int act, int device)
+{
+    if (c_in < 1 || c_out < 1 || c_in > 1 << 24 || c_out > 1 << 24) return fail(SBN_ESHAPE, "%s: channels out of range (%d, %d)", who, c_in, c_out);
+    if (act != SBN_ACT_NONE && act != SBN_ACT_RELU) return fail(SBN_EINVAL, "%s: unknown activation %d", who, act);
+    if (device < -1) return fail(SBN_EINVAL, "%s: device must be >= -1", who);
+    return SBN_OK;
+}
+
+int pack_impl(const sbn_layer_desc_t* d, int device, sbn_mx_t** out)
+{
+    const char* const who = "sbn_mx_pack";
+    if (!d || !out) return fail(SBN_EINVAL, "%s: NULL pointer", who);
+    *out = nullptr;
+    if (!d->w) return fail(SBN_EINVAL, "%s: weights pointer is NULL", who);
+    if (d->kind != SBN_CONV1X1) return fail(SBN_EINVAL, "%s: kind must be SBN_CONV1X1 (got %d)", who, d->kind);
+    if (d->stride != 1 || d->pad != 0) return fail(SBN_EINVAL, "%s: 1x1 layers need stride 1, pad 0 (got %d, %d)", who, d->stride, d->pad);
+    if (int rc = check_layer(who, d->c_in, d->c_out, d->act, device)) return rc;
+    if (d->mask) {
+        if ((d->go != 4 && d->go != 8) || (d->gi != 1 && d->gi != 2 && d->gi != 4 && d->gi != 8))
+            return fail(SBN_EINVAL, "%s: blocks of %d x %d are not supported", who, d->go, d->gi);
+        if (d->c_out % d->go || d->c_in % d->gi)
+            return fail(SBN_ESHAPE, "%s: %d x %d channels are not whole blocks of %d x %d", who, d->c_out, d->c_in, d->go, d->gi);
+    }
+    if (d->perm_out && !is_permutation(d->perm_out, d->c_out)) return fail(SBN_EPERM, "%s: perm_out is not a permutation", who);
+    if (d->perm_in && !is_permutation(d->perm_in, d->c_in)) return fail(SBN_EPERM, "%s: perm_in is not a permutation", who);
+    Holder h = make(d->c_in, d->c_out, d->act, d->bias != nullptr, device);
+    std::vector<uint8_t> codes((size_t)d->c_out * h->blocks * 16), scales((size_t)d->c_out * h->blocks);
+    std::vector<float> row(d->c_in), bias;
+    for (int r = 0; r < d->c_out; ++r) {
+        const float* const w = d->w + (size_t)(d->perm_out ? d->perm_out[r] : r) * d->c_in;
+        for (int c = 0; c < d->c_in; ++c) {
+            const float v = w[d->perm_in ? d->perm_in[c] : c];
+            const bool kept = !d->mask || d->mask[(size_t)(r / d->go) * (d->c_in / d->gi) + c / d->gi];
+            if (!std::isfinite(v)) return fail(SBN_EINVAL, "%s: weights hold NaN or infinity", who);
+            row[c] = kept ? v : 0.0f;
+        }
+        quantize_row(row.data(), d->c_in, codes.data() + (size_t)r * h->blocks * 16, scales.data() + (size_t)r * h->blocks);
+    }
+    if (d->bias) {
+        bias.resize(d->c_out);
+        for (int r = 0; r < d->c_out; ++r) bias[r] = d->bias[d->perm_out ? d->perm_out[r] : r];
+    }
+    return finish_pack(std::move(h), codes.data(), scales.data(), d->bias ? bias.data() : nullptr, out);
+}
+
+int unpack_impl(const sbn_mx_t* p, void* codes, void* scales, float* bias)
+{
+    if (!p) return fail(SBN_EINVAL, "sbn_mx_unpack: NULL pointer");
+    const size_t n = (size_t)p->c_out * p->blocks;
+    if (p->device < 0) {
+        if (codes) std::memcpy(codes, p->codes.data(), n * 16);
+        if (scales) std::memcpy(scales, p->scales.data(), n);
+        if (bias) std::memcpy(bias, p->bias.data(), (size_t)p->c_out * sizeof(float));
+        return SBN_OK;
+    }
+    DeviceScope on(p->device);
+    if (on.err != hipSuccess) return fail(SBN_EHIP, "hipSetDevice: %s", hipGetErrorString(on.err));
+    DeviceMemory staged;
+    hipError_t e = hipMalloc(&staged.p, align256(n * 16) + n);
+    if (e != hipSuccess) return fail(e == hipErrorOutOfMemory ? SBN_ENOMEM : SBN_EHIP, "hipMalloc: %s", hipGetErrorString(e));
+    uint8_t *const c = (uint8_t*)staged.p, *const s = c + align256(n * 16);
+    if (int rc = launch_mx_layout(p, nullptr, nullptr, true, c, s)) return rc;
+    if ((codes && (e = hipMemcpy(codes, c, n * 16, hipMemcpyDeviceToHost)) != hipSuccess) ||
+        (scales && (e = hipMemcpy(scales, s, n, hipMemcpyDeviceToHost)) != hipSuccess) ||
+        (bias && (e = hipMemcpy(bias, p->d_bias, (size_t)p->c_out * sizeof(float), hipMemcpyDeviceToHost)) != hipSuccess) ||
+        (e = hipDeviceSynchronize()) != hipSuccess)
+        return fail(SBN_EHIP, "sbn_mx_unpack: %s", hipGetErrorString(e));
+    return SBN_OK;
+}
+
+int linear_impl(const sbn_mx_t* p, const void* codes, const void* scales, int format, int64_t rows, void* y, int y_type, int64_t ldy,
+                void* workspace, size_t workspace_bytes, void* stream)
+{
+    const char* const who = "sbn_linear_mx";
+    if (!p) return fail(SBN_EINVAL, "%s: packed layer is NULL", who);
+    if (!is_format(format)) return fail(SBN_EINVAL, "%s: unknown format %d", who, format);
+    if (!type_bytes(y_type)) return fail(SBN_EINVAL, "%s: y has unknown type %d", who, y_type);
+    if (int rc = check_extents(who, rows, p->c_in)) return rc;
+    if (p->device < 0) return fail(SBN_ENODEV, "%s: layer was packed without a device copy", who);
+    if (rows == 0) return SBN_OK;
+    if (int rc = check_codes(who, format, codes, scales)) return rc;
+    if (int rc = check_rows(who, "y", y, y_type, p->c_out, ldy)) return rc;
+    const size_t need = linear_mx_workspace(p, format, rows);
+    if (need && (!workspace || workspace_bytes < need)) return fail(SBN_EINVAL, "%s: needs a workspace of %zu bytes (got %zu)", who, need, workspace ? workspace_bytes : 0);
+    if (need && !aligned(workspace, 16)) return fail(SBN_EINVAL, "%s: workspace must be 16-byte aligned", who);
+    int cur = -1;
+    hipError_t e = hipGetDevice(&cur);
+    if (e != hipSuccess) return fail(SBN_EHIP, "hipGetDevice: %s", hipGetErrorString(e));
+    if (cur != p->device) return fail(SBN_EINVAL, "%s: current device is %d but the layer lives on device %d", who, cur, p->device);
+    return launch_linear_mx(p, codes, scales, format, rows, y, y_type, ldy, workspace, stream);
+}
+
+int rmsnorm_impl(const sbn_rmsnorm_t* a, void* stream)
+{
+    const char* const who = "sbn_add_rmsnorm";
+    if (!a) return fail(SBN_EINVAL, "%s: NULL pointer", who);
+    if (int rc = check_extents(who, a->rows, a->cols)) return rc;
+    if (a->format && !is_format(a->format)) return fail(SBN_EINVAL, "%s: unknown format %d", who, a->format);
+    if (!(a->eps >= 0.0f)) return fail(SBN_EINVAL, "%s: eps must not be negative", who);
+    if (!type_bytes(a->x_type)) return fail(SBN_EINVAL, "%s: x has unknown type %d", who, a->x_type);
+    if (a->rows == 0) return SBN_OK;
+    if (!a->y && !a->format && !a->total) return fail(SBN_EINVAL, "%s: no output is asked for", who);
+    if (int rc = check_rows(who, "x", a->x, a->x_type, a->cols, a->ldx)) return rc;
+    if (a->residual) {
+        if (a->r_type != a->x_type && a->r_type != SBN_F32) return fail(SBN_EINVAL, "%s: the residual has x's type or SBN_F32", who);
+        if (int rc = check_rows(who, "residual", a->residual, a->r_type, a->cols, a->ldr)) return rc;
+        if (a->total)
+            if (int rc = check_rows(who, "total", a->total, a->r_type, a->cols, a->ldt)) return rc;
+        if (a->total == a->residual && a->ldt != a->ldr) return fail(SBN_EINVAL, "%s: total in the residual's place needs its row stride", who);
+        if (a->total == a->x && (a->ldt != a->ldx || a->r_type != a->x_type)) return fail(SBN_EINVAL, "%s: total in x's place needs its type and row stride", who);
+    } else if (a->total) {
+        return fail(SBN_EINVAL, "%s: total needs a residual", who);
+    }
+    if (a->weight && !aligned(a->weight, 4)) return fail(SBN_EINVAL, "%s: weight is not aligned to its type", who);
+    if (a->y) {
+        if (int rc = check_rows(who, "y", a->y, a->x_type, a->cols, a->ldy)) return rc;
+        if (a->y == a->x || a->y == a->residual || a->y == a->total) return fail(SBN_EINVAL, "%s: y must not overlap the others", who);
+    }
+    if (a->format)
+        if (int rc = check_codes(who, a->format, a->codes, a->scales)) return rc;
+    return launch_add_rmsnorm(*a, true, stream);
+}
+
+int log_probs_impl(const void* logits, int type, int64_t rows, int64_t cols, int64_t ld, const int64_t* targets, int n_targets, int k, float* logp,
+                   float* lse, float* entropy, int64_t* top_ids, float* top_logp, void* workspace, size_t workspace_bytes, void* stream)
+{
+    const char* const who = "sbn_log_probs";
+    if (int rc = check_extents(who, rows, cols)) return rc;
+    if (!type_bytes(type)) return fail(SBN_EINVAL, "%s: logits have unknown type %d", who, type);
+    if (n_targets < 0) return fail(SBN_EINVAL, "%s: negative number of targets", who);
+    if (k < 0 || k > SBN_MAX_TOP || k > cols) return fail(SBN_EINVAL, "%s: k = %d is out of range (0 to %d, and the columns)", who, k, SBN_MAX_TOP);
+    if (rows == 0) return SBN_OK;
+    if (int rc = check_rows(who, "logits", logits, type, cols, ld)) return rc;
+    if (!lse || (n_targets && (!targets || !logp)) || (k && (!top_ids || !top_logp))) return fail(SBN_EINVAL, "%s: NULL pointer", who);
+    if (!aligned(targets, 8) || !aligned(top_ids, 8) || !aligned(lse, 4) || !aligned(logp, 4) || !aligned(entropy, 4) || !aligned(top_logp, 4))
+        return fail(SBN_EINVAL, "%s: a pointer is not aligned to its type", who);
+    const size_t need = log_probs_workspace(rows, cols, k);
+    if (need && (!workspace || workspace_bytes < need)) return fail(SBN_EINVAL, "%s: needs a workspace of %zu bytes (got %zu)", who, need, workspace ? workspace_bytes : 0);
+    if (need && !aligned(workspace, 16)) return fail(SBN_EINVAL, "%s: workspace must be 16-byte aligned", who);
+    return launch_log_probs(logits, type, rows, cols, ld, targets, n_targets, k, logp, lse, entropy, top_ids, top_logp, workspace, stream);
+}
+
+int log_probs_backward_impl(const void* logits, int type, int64_t rows, int64_t cols, int64_t ld, const int64_t* targets, int n_targets,
+                            const float* lse, const float* entropy, const float* g_logp, const float* g_entropy, void* grad, int64_t ldg, void* stream)
+{
+    const char* const who = "sbn_log_probs_backward";
+    if (int rc = check_extents(who, rows, cols)) return rc;
+    if (!type_bytes(type)) return fail(SBN_EINVAL, "%s: logits have unknown type %d", who, type);
+    if (n_targets < 0) return fail(SBN_EINVAL, "%s: negative number of targets", who);
+    if (rows == 0) return SBN_OK;
+    if (int rc = check_rows(who, "logits", logits, type, cols, ld)) return rc;
+    if (int rc = check_rows(who, "grad", grad, type, cols, ldg)) return rc;
+    if (grad == logits && ldg != ld) return fail(SBN_EINVAL, "%s: a gradient in the logits' place needs their row stride", who);
+    if (!lse || (n_targets && (!targets || !g_logp)) || (g_entropy && !entropy)) return fail(SBN_EINVAL, "%s: NULL pointer", who);
+    if (!aligned(targets, 8) || !aligned(lse, 4) || !aligned(entropy, 4) || !aligned(g_logp, 4) || !aligned(g_entropy, 4))
+        return fail(SBN_EINVAL, "%s: a pointer is not aligned to its type", who);
+    return launch_log_probs_backward(logits, type, rows, cols, ld, targets, n_targets, lse, entropy, g_logp, g_entropy, grad, ldg, stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+int sbn_quantized_bytes(int format, int64_t rows, int64_t cols, size_t* code_bytes, size_t* scale_bytes)
+{
+    clear_error();
+    if (!is_format(format)) return fail(SBN_EINVAL, "sbn_quantized_bytes: unknown format %d", format);
+    if (int rc = check_extents("sbn_quantized_bytes", rows, cols)) return rc;
+    const size_t blocks = ((size_t)cols + 31) / 32;
+    if (code_bytes) *code_bytes = (size_t)rows * blocks * (format == SBN_MXFP4 ? 16 : 32);
+    if (scale_bytes) *scale_bytes = (size_t)rows * (format == SBN_FP8_ROW ? sizeof(float) : blocks);
+    return SBN_OK;
+}
+
+int sbn_quantize(const void* x, int x_type, int64_t rows, int64_t cols, int64_t ldx, int format, void* codes, void* scales, void* stream)
+{
+    clear_error();
+    return guarded("sbn_quantize", [&]() -> int {
+        if (!is_format(format)) return fail(SBN_EINVAL, "sbn_quantize: unknown format %d", format);
+        if (!type_bytes(x_type)) return fail(SBN_EINVAL, "sbn_quantize: x has unknown type %d", x_type);
+        if (int rc = check_extents("sbn_quantize", rows, cols)) return rc;
+        if (rows == 0) return SBN_OK;
+        if (int rc = check_rows("sbn_quantize", "x", x, x_type, cols, ldx)) return rc;
+        if (int rc = check_codes("sbn_quantize", format, codes, scales)) return rc;
+        return launch_quantize(x, x_type, rows, cols, ldx, format, codes, scales, stream);
+    });
+}
+
+int sbn_dequantize(const void* codes, const void* scales, int format, int64_t rows, int64_t cols, void* y, int y_type, int64_t ldy, void* stream)
+{
+    clear_error();
+    return guarded("sbn_dequantize", [&]() -> int {
+        if (!is_format(format)) return fail(SBN_EINVAL, "sbn_dequantize: unknown format %d", format);
+        if (!type_bytes(y_type)) return fail(SBN_EINVAL, "sbn_dequantize: y has unknown type %d", y_type);
+        if (int rc = check_extents("sbn_dequantize", rows, cols)) return rc;
+        if (rows == 0) return SBN_OK;
+        if (int rc = check_codes("sbn_dequantize", format, codes, scales)) return rc;
+        if (int rc = check_rows("sbn_dequantize", "y", y, y_type, cols, ldy)) return rc;
+        return launch_dequantize(codes, scales, format, rows, cols, y, y_type, ldy, stream);
+    });
+}
+
+int sbn_add_rmsnorm(const sbn_rmsnorm_t* a, void* stream)
+{
+    clear_error();
+    return guarded("sbn_add_rmsnorm", [&]() -> int { return rmsnorm_impl(a, stream); });
+}
+
+int sbn_mx_pack(const sbn_layer_desc_t* d, int device, sbn_mx_t** out)
+{
+    clear_error();
+    return guarded("sbn_mx_pack", [&]() -> int { return pack_impl(d, device, out); });
+}
+
+int sbn_mx_pack_codes(const void* codes, const void* scales, int c_in, int c_out, const float* bias, int act, int device, sbn_mx_t** out)
+{
+    clear_error();
+    return guarded("sbn_mx_pack_codes", [&]() -> int {
+        if (!codes || !scales || !out) return fail(SBN_EINVAL, "sbn_mx_pack_codes: NULL pointer");
+        *out = nullptr;
+        if (int rc = check_layer("sbn_mx_pack_codes", c_in, c_out, act, device)) return rc;
+        return finish_pack(make(c_in, c_out, act, bias != nullptr, device), codes, scales, bias, out);
+    });
+}
+
+int sbn_mx_unpack(const sbn_mx_t* p, void* codes, void* scales, float* bias)
+{
+    clear_error();
+    return guarded("sbn_mx_unpack", [&]() -> int { return unpack_impl(p, codes, scales, bias); });
+}
+
+int sbn_mx_info(const sbn_mx_t* p, int* c_in, int* c_out, int* act, int* device, size_t* device_bytes)
+{
+    clear_error();
+    if (!p) return fail(SBN_EINVAL, "sbn_mx_info: NULL pointer");
+    if (c_in) *c_in = p->c_in;
+    if (c_out) *c_out = p->c_out;
+    if (act) *act = p->act;
+    if (device) *device = p->device;
+    if (device_bytes) *device_bytes = p->device_bytes;
+    return SBN_OK;
+}
+
+void sbn_mx_free(sbn_mx_t* p) { release(p); }
+
+int sbn_linear_mx_workspace(const sbn_mx_t* p, int format, int64_t rows, size_t* bytes)
+{
+    clear_error();
+    if (!p || !bytes) return fail(SBN_EINVAL, "sbn_linear_mx_workspace: NULL pointer");
+    if (!is_format(format)) return fail(SBN_EINVAL, "sbn_linear_mx_workspace: unknown format %d", format);
+    if (int rc = check_extents("sbn_linear_mx_workspace", rows, p->c_in)) return rc;
+    *bytes = linear_mx_workspace(p, format, rows);
+    return SBN_OK;
+}
+
+int sbn_linear_mx(const sbn_mx_t* p, const void* codes, const void* scales, int format, int64_t rows, void* y, int y_type, int64_t ldy,
+                  void* workspace, size_t workspace_bytes, void* stream)
+{
+    clear_error();
+    return guarded("sbn_linear_mx", [&]() -> int { return linear_impl(p, codes, scales, format, rows, y, y_type, ldy, workspace, workspace_bytes, stream); });
+}
+
+int sbn_log_probs_workspace(int64_t rows, int64_t cols, int k, size_t* bytes)
+{
+    clear_error();
+    if (!bytes) return fail(SBN_EINVAL, "sbn_log_probs_workspace: NULL pointer");
+    if (int rc = check_extents("sbn_log_probs_workspace", rows, cols)) return rc;
+    if (k < 0 || k > SBN_MAX_TOP || k > cols) return fail(SBN_EINVAL, "sbn_log_probs_workspace: k = %d is out of range", k);
+    *bytes = log_probs_workspace(rows, cols, k);
+    return SBN_OK;
+}
+
+int sbn_log_probs(const void* logits, int type, int64_t rows, int64_t cols, int64_t ld, const int64_t* targets, int n_targets, int k, float* logp,
+                  float* lse, float* entropy, int64_t* top_ids, float* top_logp, void* workspace, size_t workspace_bytes, void* stream)
+{
+    clear_error();
+    return guarded("sbn_log_probs", [&]() -> int {
+        return log_probs_impl(logits, type, rows, cols, ld, targets, n_targets, k, logp, lse, entropy, top_ids, top_logp, workspace, workspace_bytes, stream);
+    });
+}
+
+int sbn_log_probs_backward(const void* logits, int type, int64_t rows, int64_t cols, int64_t ld, const int64_t* targets, int n_targets,
+                           const float* lse, const float* entropy, const float* g_logp, const float* g_entropy, void* grad, int64_t ldg, void* stream)
+{
+    clear_error();
+    return guarded("sbn_log_probs_backward", [&]() -> int {
+        return log_probs_backward_impl(logits, type, rows, cols, ld, targets, n_targets, lse, entropy, g_logp, g_entropy, grad, ldg, stream);
+    });
+}
+
+}  // extern "C"

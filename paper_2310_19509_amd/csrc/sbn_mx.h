@@ -1,0 +1,45 @@
+// Layers with weights in microscaled 4 bits: what the packer and the kernels share.
+#pragma once
+#include <vector>
+
+#include "sbn_internal.h"
+
+// Device layout.  A TILE is 16 output channels x 128 input channels, the A operand of one 16 x 16 x 128 multiply as it lies in
+// registers: lane l holds channel l % 16, inputs 32 (l / 16) .. + 31 of the 128 (one block, 16 bytes, even input low), so that a
+// wave fetches a tile with one 16-byte load per lane from 1024 consecutive bytes:
+//     codes [tile row][step][lane 64][16 bytes]         steps = ceil(c_in / 128), tile rows = ceil(c_out / 16)
+// and lane l's scales of four consecutive steps are the bytes of one word:
+//     scales [tile row][quad][lane 64][4 bytes]         quads = ceil(steps / 4)
+// Past c_in and c_out: codes 0, scale byte 0.
+struct sbn_mx {
+    int c_in = 0, c_out = 0, act = 0, device = -1;
+    bool has_bias = false;
+    int blocks = 0, steps = 0, quads = 0, tile_rows = 0;
+    std::vector<uint8_t> codes, scales;       // host copy [c_out][blocks * 16], [c_out][blocks] (device = -1 only)
+    std::vector<float> bias;                  // likewise [c_out]
+    void* d_blob = nullptr;
+    uint8_t* d_codes = nullptr;
+    uint8_t* d_scales = nullptr;
+    float* d_bias = nullptr;                  // [tile_rows * 16], zeros without a bias
+    size_t device_bytes = 0;
+    int cus = 256;
+};
+
+namespace sbn {
+
+// codes / scales (device, row-major) into the layout above; synchronous errors only
+int launch_mx_layout(const sbn_mx* p, const uint8_t* codes, const uint8_t* scales, bool back, uint8_t* codes_out, uint8_t* scales_out);
+size_t linear_mx_workspace(const sbn_mx* p, int format, long long rows);
+int launch_linear_mx(const sbn_mx* p, const void* codes, const void* scales, int format, long long rows, void* y, int y_type, long long ldy,
+                     void* workspace, void* stream);
+
+int launch_quantize(const void* x, int x_type, long long rows, long long cols, long long ldx, int format, void* codes, void* scales, void* stream);
+int launch_dequantize(const void* codes, const void* scales, int format, long long rows, long long cols, void* y, int y_type, long long ldy, void* stream);
+int launch_add_rmsnorm(const sbn_rmsnorm_t& n, bool norm, void* stream);
+size_t log_probs_workspace(long long rows, long long cols, int k);
+int launch_log_probs(const void* logits, int type, long long rows, long long cols, long long ld, const int64_t* targets, int n_targets, int k,
+                     float* logp, float* lse, float* entropy, int64_t* top_ids, float* top_logp, void* workspace, void* stream);
+int launch_log_probs_backward(const void* logits, int type, long long rows, long long cols, long long ld, const int64_t* targets, int n_targets,
+                              const float* lse, const float* entropy, const float* g_logp, const float* g_entropy, void* grad, long long ldg, void* stream);
+
+}  // namespace sbn

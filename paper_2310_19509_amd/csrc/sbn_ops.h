@@ -1,0 +1,202 @@
+// Device helpers shared by the low-precision and scoring kernels: element types at any alignment,
+// codes of the 4- and 8-bit formats.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "sbn_internal.h"
+
+namespace sbn {
+
+// log2 of the largest element's power of two, and the saturation value, of the two element types
+constexpr int kEmax4 = 2, kEmax8 = 8;
+constexpr float kTop8 = 448.0f;
+constexpr float kLeastRow = 6.018531e-36f;            // 2^-117: below it 448 / a leaves 32 bits
+
+#ifdef __HIPCC__
+
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f2 __attribute__((ext_vector_type(2)));
+typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef unsigned u4 __attribute__((ext_vector_type(4)));
+typedef unsigned u2 __attribute__((ext_vector_type(2)));
+typedef short s2 __attribute__((ext_vector_type(2)));
+
+// 16 bytes at the alignment of their elements: rows of odd length begin anywhere, and global memory takes wide
+// accesses there, so one form of load serves all strides.
+struct __attribute__((packed, aligned(2))) Any16 { u4 v; };
+struct __attribute__((packed, aligned(2))) Any8 { u2 v; };
+
+template <class T> struct Elem;
+template <> struct Elem<float> {
+    static __device__ float get(float v) { return v; }
+    static __device__ float put(float v) { return v; }
+};
+template <> struct Elem<__bf16> {
+    static __device__ float get(__bf16 v) { return (float)v; }
+    static __device__ __bf16 put(float v) { return (__bf16)v; }
+};
+template <> struct Elem<_Float16> {
+    static __device__ float get(_Float16 v) { return (float)v; }
+    static __device__ _Float16 put(float v) { return (_Float16)v; }
+};
+
+// Eight consecutive elements as they lie in memory, and as 32-bit values.
+template <class T> struct Raw {
+    u4 w[sizeof(T) / 2];
+};
+template <class T>
+__device__ inline Raw<T> fetch(const T* p)
+{
+    Raw<T> r;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = ((const Any16*)p)[i].v;
+    return r;
+}
+__device__ inline void expand(const Raw<float>& r, float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const unsigned u = r.w[i >> 2][i & 3];            // (a copy: bit casts of a vector's element take its first one)
+        v[i] = __builtin_bit_cast(float, u);
+    }
+}
+__device__ inline void expand(const Raw<__bf16>& r, float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        v[2 * i] = __builtin_bit_cast(float, r.w[0][i] << 16), v[2 * i + 1] = __builtin_bit_cast(float, r.w[0][i] & 0xFFFF0000u);
+}
+__device__ inline void expand(const Raw<_Float16>& r, float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned u = r.w[0][i];
+        const h2 h = __builtin_bit_cast(h2, u);
+        v[2 * i] = (float)h.x, v[2 * i + 1] = (float)h.y;
+    }
+}
+// Columns 8 unit .. + 7 of a row, in two steps so that several loads are under way before the first is used: all lanes
+// load eight elements (those past the row's end its last eight, when it has as many), and the lanes at the end
+// correct what they have.
+template <class T>
+__device__ inline Raw<T> fetch_unit(const T* row, long long unit, long long cols)
+{
+    return cols >= 8 ? fetch(row + min(unit * 8, cols - 8)) : Raw<T>{};
+}
+template <class T>
+__device__ inline void expand_unit(const Raw<T>& r, const T* row, long long unit, long long cols, float (&v)[8], float rest)
+{
+    expand(r, v);
+    const long long left = cols - unit * 8;
+    if (left < 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < left ? Elem<T>::get(row[unit * 8 + i]) : rest;
+    }
+}
+__device__ inline void store8(float* p, const float (&v)[8])
+{
+    u4 a, b;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = __builtin_bit_cast(unsigned, v[i]), b[i] = __builtin_bit_cast(unsigned, v[4 + i]);
+    ((Any16*)p)[0].v = a, ((Any16*)p)[1].v = b;
+}
+__device__ inline void store8(__bf16* p, const float (&v)[8])
+{
+    u4 a;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = __builtin_bit_cast(unsigned, __builtin_convertvector((f2){v[2 * i], v[2 * i + 1]}, b2));
+    ((Any16*)p)->v = a;
+}
+__device__ inline void store8(_Float16* p, const float (&v)[8])
+{
+    u4 a;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = __builtin_bit_cast(unsigned, __builtin_convertvector((f2){v[2 * i], v[2 * i + 1]}, h2));
+    ((Any16*)p)->v = a;
+}
+// Eight values to columns 8 unit .. + 7 of a row, as many as it has.
+template <class T>
+__device__ inline void store_unit(T* row, long long unit, long long cols, const float (&v)[8])
+{
+    T* const p = row + unit * 8;
+    const long long left = cols - unit * 8;
+    if (left >= 8) {
+        store8(p, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < left) p[i] = Elem<T>::put(v[i]);
+    }
+}
+
+// The bits of the largest magnitude: ordered as integers, NaN above infinity above every number.
+__device__ inline unsigned top_bits(const float (&v)[8])
+{
+    unsigned t = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t = max(t, __builtin_bit_cast(unsigned, v[i]) & 0x7FFFFFFFu);
+    return t;
+}
+// Scale byte of a block from that; 2^(byte - 127).
+template <int EMAX>
+__device__ inline int scale_byte(unsigned top)
+{
+    const int e = (int)(top >> 23);
+    return e == 255 ? 255 : max(e - EMAX, 0);
+}
+__device__ inline float scale_of(int byte) { return __builtin_bit_cast(float, byte ? (unsigned)byte << 23 : 0x00400000u); }
+
+// Eight values to E2M1 codes (even column low) / E4M3 codes, divided by a power of two on the way; the 4-bit conversion
+// saturates, the 8-bit one makes NaN of what is too large, so it gets its range first.
+__device__ inline unsigned codes4(const float (&v)[8], float scale)
+{
+    unsigned c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0], v[1], scale, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2], v[3], scale, 1);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4], v[5], scale, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6], v[7], scale, 3);
+}
+__device__ inline float in8(float v, float top) { return __builtin_amdgcn_fmed3f(v, -top, top); }
+__device__ inline u2 codes8(const float (&v)[8], float scale)
+{
+    const float t = kTop8 * scale;
+    u2 r;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        s2 c = {};
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, in8(v[4 * h], t), in8(v[4 * h + 1], t), scale, false);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(c, in8(v[4 * h + 2], t), in8(v[4 * h + 3], t), scale, true);
+        r[h] = __builtin_bit_cast(unsigned, c);
+    }
+    return r;
+}
+
+__device__ inline float wave_sum(float v)
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+    return v;
+}
+__device__ inline float wave_max(float v)
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+    return v;
+}
+__device__ inline unsigned wave_max(unsigned v)
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) v = max(v, (unsigned)__shfl_xor((int)v, d));
+    return v;
+}
+// The largest of four neighbouring lanes: the 32 columns of a block.
+__device__ inline unsigned quad_max(unsigned v)
+{
+    v = max(v, (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true));   // lanes 1 0 3 2
+    return max(v, (unsigned)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true));   // lanes 2 3 0 1
+}
+
+#endif  // __HIPCC__
+
+}  // namespace sbn

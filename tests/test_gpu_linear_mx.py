@@ -1,0 +1,178 @@
+"""The product with 4-bit weights against the definition in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2310_19509_amd as S
+from oracle import lowp as L
+
+pytestmark = pytest.mark.gpu
+FORMATS = [S.SBN_MXFP4, S.SBN_MXFP8, S.SBN_FP8_ROW]
+# half a unit in the last place over the least value of its binade: 2^-(significant bits)
+HALF_ULP = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+
+
+def _rows(seed, rows, cols, fmt, dtype=torch.bfloat16):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn((rows, cols), device="cuda", generator=g)
+    x = torch.where(torch.rand(cols, device="cuda", generator=g) < 0.02, x * 20, x).to(dtype)
+    codes, scales = S.sbn_quantized_empty(fmt, rows, cols)
+    S.sbn_quantize(x, fmt, codes, scales)
+    return codes, scales
+
+
+def _layer(seed, n, k, bias, act):
+    rng = np.random.default_rng(seed)
+    w = (rng.standard_normal((n, k)) / np.sqrt(k)).astype(np.float32)
+    b = rng.standard_normal(n).astype(np.float32) if bias else None
+    p = S.sbn_mx_pack(w, bias=b, act=act)
+    codes, scales, _ = S.sbn_mx_unpack(p)
+    return p, L.values(codes, scales, L.MXFP4, k), np.zeros(n) if b is None else b.astype(np.float64)
+
+
+def _run(p, codes, scales, fmt, rows, dtype, pad=0, stream=None):
+    y = torch.full((rows, p.c_out + pad), 7.0, dtype=dtype, device="cuda")
+    n = S.sbn_linear_mx_workspace(p, fmt, rows)
+    ws = torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda") if n else None
+    S.sbn_linear_mx(p, codes, scales, fmt, y[:, :p.c_out], workspace=ws, stream=stream)
+    assert (y[:, p.c_out:] == 7).all()
+    return y[:, :p.c_out]
+
+
+def _bound(x, w, fmt, dtype):
+    """Sums of products of at most 8 significant bits in 32 bits: 2^-24 for every addition of a running sum of 32 products (and 8 to join the
+    parts).  16-bit results of 8-bit rows may come from multiplies that cut products of 128 at 2^-13 of the largest: that is for their sum's size."""
+    k = x.shape[1]
+    rel = 2.0 ** -24 * (k / 32 + 16)
+    if dtype != torch.float32 and fmt != S.SBN_MXFP4:
+        rel += 2.0 ** -13
+    return rel * (np.abs(x) @ np.abs(w).T)
+
+
+def _check(y, x, w, b, act, fmt, dtype):
+    want = x @ w.T + b
+    tol = _bound(x, w, fmt, dtype)
+    if act == S.SBN_ACT_RELU:
+        want = np.maximum(want, 0)
+    got = y.double().cpu().numpy()
+    tol = tol + np.abs(want) * (HALF_ULP[dtype] * 1.01 + 2.0 ** -22) + np.abs(b) * 2.0 ** -22 + (2.0 ** -24 if dtype == torch.float16 else 0)
+    assert np.all(np.abs(got - want) <= tol), float((np.abs(got - want) / tol).max())
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("rows,k,n,bias,act", [(1, 1, 1, False, 0), (1, 33, 17, True, 0), (2, 128, 16, False, 1), (3, 127, 15, True, 1), (16, 512, 64, False, 0), (17, 1000, 100, True, 0),
+                                               (31, 640, 257, False, 0), (64, 256, 128, True, 1), (65, 129, 130, False, 0), (128, 1024, 256, False, 0), (200, 2051, 300, True, 0),
+                                               (257, 384, 513, False, 0), (300, 96, 1000, True, 1), (1, 4096, 2000, True, 0), (7, 9000, 48, False, 0), (520, 1536, 520, False, 0)])
+def test_against_64_bits(fmt, dtype, rows, k, n, bias, act):
+    p, w, b = _layer(rows + k + n, n, k, bias, act)
+    codes, scales = _rows(rows * k, rows, k, fmt)
+    x = L.values(codes.cpu().numpy(), scales.cpu().numpy(), fmt, k)
+    y = _run(p, codes, scales, fmt, rows, dtype, pad=(rows + n) % 3)
+    _check(y, x, w, b, act, fmt, dtype)
+    assert torch.equal(y, _run(p, codes, scales, fmt, rows, dtype))       # the same bits each time
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("rows", [1, 40, 300])
+def test_every_weight_counts_where_it_lies(fmt, rows):
+    """One column of X at a time would take long: powers of two along the columns make every product's place visible in the sum's exact value."""
+    k, n = 224, 80
+    rng = np.random.default_rng(0)
+    wc = rng.integers(0, 8, (n, k))                                      # codes 0 .. 7
+    codes = (wc[:, 0::2] | wc[:, 1::2] << 4).astype(np.uint8)
+    ws = rng.integers(125, 130, (n, k // 32)).astype(np.uint8)
+    p = S.sbn_mx_pack_codes(codes, ws, k)
+    x = (rng.integers(0, 2, (rows, k)) * rng.integers(1, 4, (rows, k))).astype(np.float32)
+    xc, xs = S.sbn_quantized_empty(fmt, rows, k)
+    if fmt == S.SBN_FP8_ROW:
+        x[:, 0] = 3.5                                                    # a scale of 2^-7
+    S.sbn_quantize(torch.from_numpy(x).cuda(), fmt, xc, xs)
+    xv = L.values(xc.cpu().numpy(), xs.cpu().numpy(), fmt, k)
+    assert np.array_equal(xv, x)
+    y = _run(p, xc, xs, fmt, rows, torch.float32)
+    assert np.array_equal(y.double().cpu().numpy(), x.astype(np.float64) @ L.values(codes, ws, L.MXFP4, k).T)     # small whole multiples: exact
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("rows", [5, 150])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_nan_stays_in_its_row_and_channel(fmt, rows, dtype):
+    k, n = 300, 140
+    rng = np.random.default_rng(1)
+    codes, scales = rng.integers(0, 256, (n, 160), dtype=np.uint8), rng.integers(120, 130, (n, 10), dtype=np.uint8)
+    scales[70, 3] = 255
+    p = S.sbn_mx_pack_codes(codes, scales, k)
+    x = torch.randn(rows, k, device="cuda")
+    x[2, 250] = float("nan")
+    x[4, 17] = float("inf")
+    xc, xs = S.sbn_quantized_empty(fmt, rows, k)
+    S.sbn_quantize(x, fmt, xc, xs)
+    bad = torch.isnan(_run(p, xc, xs, fmt, rows, dtype)).cpu().numpy()
+    want = np.zeros((rows, n), dtype=bool)
+    want[[2, 4]] = True
+    want[:, 70] = True
+    assert np.array_equal(bad, want)
+
+
+@pytest.mark.parametrize("rows", [1, 30, 400])
+def test_masked_rearranged_layer_and_device_codes(rows):
+    rng = np.random.default_rng(8)
+    n, k = 96, 160
+    w = rng.standard_normal((n, 1, 1, k)).astype(np.float32)
+    po, pi = rng.permutation(n).astype(np.int32), rng.permutation(k).astype(np.int32)
+    mask = S.sbn_prune_magnitude(np.ascontiguousarray(w[po][..., pi]), S.SBN_CONV1X1, 4, 4, 60)
+    bias = rng.standard_normal(n).astype(np.float32)
+    p = S.sbn_mx_pack(w, mask=mask, bias=bias, perm_out=po, perm_in=pi, act=S.SBN_ACT_RELU)
+    wq = L.values(*L.quantize((w[po][..., pi].reshape(n, k) * np.kron(mask, np.ones((4, 4)))).astype(np.float64), L.MXFP4), L.MXFP4, k)
+    codes, scales = _rows(3, rows, k, S.SBN_MXFP8)
+    y = _run(p, codes, scales, S.SBN_MXFP8, rows, torch.float32)
+    _check(y, L.values(codes.cpu().numpy(), scales.cpu().numpy(), L.MXFP8, k), wq, bias[po].astype(np.float64), S.SBN_ACT_RELU, S.SBN_MXFP8, torch.float32)
+    c, s, b = S.sbn_mx_unpack(p)
+    q = S.sbn_mx_pack_codes(torch.from_numpy(c).cuda(), torch.from_numpy(s).cuda(), k, bias=torch.from_numpy(b).cuda(), act=S.SBN_ACT_RELU)
+    assert all(np.array_equal(u, v) for u, v in zip(S.sbn_mx_unpack(q), (c, s, b)))
+    assert torch.equal(_run(q, codes, scales, S.SBN_MXFP8, rows, torch.float32), y)
+    assert S.sbn_mx_info(q)["device_bytes"] > 0
+
+
+def test_relu_of_nan_is_zero():
+    codes, scales = np.zeros((16, 16), dtype=np.uint8), np.full((16, 1), 255, dtype=np.uint8)
+    p = S.sbn_mx_pack_codes(codes, scales, 32, act=S.SBN_ACT_RELU)
+    for rows in (1, 200):
+        xc, xs = _rows(1, rows, 32, S.SBN_MXFP4)
+        assert (_run(p, xc, xs, S.SBN_MXFP4, rows, torch.float32) == 0).all()
+
+
+def test_output_rows_far_apart():
+    p, w, b = _layer(5, 48, 100, True, 0)
+    ld = 3 << 29
+    y = torch.empty(2 * ld + 4096, dtype=torch.bfloat16, device="cuda").as_strided((3, 48), (ld, 1))
+    codes, scales = _rows(3, 3, 100, S.SBN_MXFP8)
+    n = S.sbn_linear_mx_workspace(p, S.SBN_MXFP8, 3)
+    S.sbn_linear_mx(p, codes, scales, S.SBN_MXFP8, y, workspace=torch.empty(n, dtype=torch.uint8, device="cuda") if n else None)
+    assert torch.equal(y, _run(p, codes, scales, S.SBN_MXFP8, 3, torch.bfloat16))
+
+
+def test_streams_no_rows_and_refusals():
+    p, w, b = _layer(6, 64, 256, False, 0)
+    codes, scales = _rows(4, 33, 256, S.SBN_MXFP4)
+    want = _run(p, codes, scales, S.SBN_MXFP4, 33, torch.float32)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = _run(p, codes, scales, S.SBN_MXFP4, 33, torch.float32)
+    side.synchronize()
+    assert torch.equal(got, want)
+    S.sbn_linear_mx(p, codes[:0], scales[:0], S.SBN_MXFP4, torch.empty(0, 64, device="cuda"))
+    y = torch.empty(33, 64, device="cuda")
+    for bad in (lambda: S.sbn_linear_mx(p, codes, scales, S.SBN_MXFP8, y), lambda: S.sbn_linear_mx(p, codes, scales, S.SBN_MXFP4, y[:, :63]),
+                lambda: S.sbn_linear_mx(p, codes, scales, S.SBN_MXFP4, y[:32]), lambda: S.sbn_linear_mx(p, codes.cpu(), scales, S.SBN_MXFP4, y),
+                lambda: S.sbn_linear_mx(p, codes, scales, S.SBN_MXFP4, y.double())):
+        with pytest.raises(ValueError):
+            bad()
+    assert S.sbn_mx_pack(np.zeros((4, 4), dtype=np.float32), device=-1).device == -1
+    with pytest.raises(S.SbnError) as e:
+        S.sbn_linear_mx(S.sbn_mx_pack(np.zeros((4, 32), dtype=np.float32), device=-1), *_rows(4, 1, 32, S.SBN_MXFP4), S.SBN_MXFP4, torch.empty(1, 4, device="cuda"))
+    assert e.value.code == -6
+    with pytest.raises(S.SbnError):
+        S.sbn_mx_pack(np.zeros((4, 4), dtype=np.float32), device=99)
