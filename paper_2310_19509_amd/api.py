@@ -10,7 +10,7 @@ from . import _lib
 from ._lib import ChainItem, LayerDesc
 
 __all__ = [
-    "SBN_CONV1X1", "SBN_CONV3X3", "SBN_ACT_NONE", "SBN_ACT_RELU",
+    "SBN_CONV1X1", "SBN_CONV3X3", "SBN_LINEAR_MX", "SBN_ACT_NONE", "SBN_ACT_RELU",
     "SBN_ITEM_SPARSE", "SBN_ITEM_DW3X3", "SBN_ITEM_AVGPOOL", "SbnError", "Packed", "Chain",
     "sbn_last_error", "sbn_prune_magnitude", "sbn_retained_l1", "sbn_rearrange", "sbn_rearrange_graph", "sbn_order_groups", "sbn_order_groups_graph", "sbn_packed_layout", "sbn_pack", "sbn_unpack",
     "sbn_export", "sbn_packed_info", "sbn_packed_work", "sbn_free", "sbn_conv1x1_sparse", "sbn_conv3x3_sparse",
@@ -26,7 +26,7 @@ __all__ = [
     "sbn_log_probs_workspace", "sbn_log_probs", "sbn_log_probs_backward",
 ]
 
-SBN_CONV1X1, SBN_CONV3X3 = 1, 3
+SBN_CONV1X1, SBN_CONV3X3, SBN_LINEAR_MX = 1, 3, 4
 SBN_ACT_NONE, SBN_ACT_RELU = 0, 1
 SBN_ITEM_SPARSE, SBN_ITEM_DW3X3, SBN_ITEM_AVGPOOL, SBN_ITEM_STEM3X3 = 1, 2, 3, 4
 SBN_DW_PATTERN_DENSE = 8
@@ -178,7 +178,7 @@ def sbn_dw_pattern_apply(w, pattern, go: int = 16) -> np.ndarray:
 
 
 def sbn_force_kernel_form(kind: int, form: int) -> None:
-    """Force one form of the 1x1 or 3x3 kernel for all later launches (0 = automatic); for tests."""
+    """Force one form of the 1x1, 3x3 or 4-bit kernel for all later launches (0 = automatic); for tests."""
     _check(_lib.lib().sbn_force_kernel_form(int(kind), int(form)))
 
 

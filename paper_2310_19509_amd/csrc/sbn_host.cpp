@@ -30,8 +30,9 @@ int fail(int code, const char* fmt, ...)
 void clear_error() { g_err.clear(); }
 
 // kernel form forced by sbn_force_kernel_form, per layer kind; 0 = chosen per launch
-static std::atomic<int> g_form1x1{0}, g_form3x3{0};
-int forced_kernel_form(int kind) { return (kind == SBN_CONV3X3 ? g_form3x3 : g_form1x1).load(std::memory_order_relaxed); }
+static std::atomic<int> g_form1x1{0}, g_form3x3{0}, g_form_mx{0};
+static std::atomic<int>& form_of(int kind) { return kind == SBN_CONV3X3 ? g_form3x3 : kind == SBN_LINEAR_MX ? g_form_mx : g_form1x1; }
+int forced_kernel_form(int kind) { return form_of(kind).load(std::memory_order_relaxed); }
 
 bool is_permutation(const int32_t* p, int n)
 {
@@ -378,15 +379,18 @@ int sbn_force_kernel_form(int kind, int form)
 {
     clear_error();
     static const int forms1x1[] = {0, 1, 11, 12, 14, 21, 22, 112, 121, 402, 404, 504, 508, 516, 1012, 1021, 1112, 1121, 2032, 2064, 2256, 3004, 3008}, forms3x3[] = {0, 1, 2, 3, 32, 2064, 2065, 2128, 3004, 3008, 3016};
+    static const int forms_mx[] = {0, 1, 44, 88};
     bool ok = false;
     if (kind == SBN_CONV1X1)
         for (int f : forms1x1) ok |= f == form;
     else if (kind == SBN_CONV3X3)
         for (int f : forms3x3) ok |= f == form;
+    else if (kind == SBN_LINEAR_MX)
+        for (int f : forms_mx) ok |= f == form;
     else
-        return fail(SBN_EINVAL, "sbn_force_kernel_form: kind must be SBN_CONV1X1 or SBN_CONV3X3 (got %d)", kind);
+        return fail(SBN_EINVAL, "sbn_force_kernel_form: kind must be SBN_CONV1X1, SBN_CONV3X3 or SBN_LINEAR_MX (got %d)", kind);
     if (!ok) return fail(SBN_EINVAL, "sbn_force_kernel_form: %d is not a kernel form of this kind", form);
-    (kind == SBN_CONV3X3 ? sbn::g_form3x3 : sbn::g_form1x1).store(form, std::memory_order_relaxed);
+    sbn::form_of(kind).store(form, std::memory_order_relaxed);
     return SBN_OK;
 }
 

@@ -90,6 +90,18 @@ __device__ inline b8 wide8(unsigned lo, unsigned hi, float scale)
     return (b8){a.x, a.y, b.x, b.y, d.x, d.y, e.x, e.y};
 }
 
+// 16 x 16 x 128 with byte s of the scale words; BL: what the rows are (4: E2M1, 0: E4M3).  s is known once the caller's loops are unrolled.
+template <int BL>
+__device__ inline f4 scaled_mma(i8v a, i8v b, f4 c, int s, unsigned sa, unsigned sb)
+{
+    switch (s) {
+    case 0: return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4, BL, 0, (int)sa, 0, (int)sb);
+    case 1: return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4, BL, 1, (int)sa, 1, (int)sb);
+    case 2: return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4, BL, 2, (int)sa, 2, (int)sb);
+    default: return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 4, BL, 3, (int)sa, 3, (int)sb);
+    }
+}
+
 // Four consecutive output channels of a row.
 template <class T>
 __device__ inline void put4(T* y, int n, f4 v)
@@ -189,6 +201,192 @@ __global__ __launch_bounds__(256) void rows_kernel(const LinearArgs a)
             if (tile0 + t < a.tile_rows) finish4<FMT, T>(a, row, (tile0 + t) * 16 + g * 4, acc[t] + sums[0][t][lane] + sums[1][t][lane] + sums[2][t][lane]);
 }
 
+// Tiles: CH = 32 MT output channels x RW = 32 NT rows to a workgroup of 2 x 2 waves, each 16 MT x 16 NT.
+//
+// Weights go from memory straight to registers (a tile of the layout is one 16-byte load per lane), one step of 128 input channels
+// ahead.  Rows go through LDS in stages of 128 bytes of codes (two steps of 4-bit codes, one of 8-bit ones), two buffers: while a
+// stage is multiplied, the next one moves from registers to LDS and the one after it from memory to registers, so one barrier a
+// stage is enough.  Sixteen-byte pieces of a row lie at piece ^ (row & 7), which spreads the reads of eight rows over all banks.
+// The last quad's steps past c_in multiply zeros: leaving the loop among them would cost registers for every sum.
+// Scales of rows are turned, four steps at a time, into words that hold a lane's bytes of four steps, as the weights' are.
+enum { kNarrow, kScaled8, kWide8 };         // 4-bit rows; 8-bit rows on scaled multiplies; 8-bit rows as bfloat16
+template <int MODE, bool BLOCKS, class T, int MT, int NT>
+__global__ __launch_bounds__(256, MT * NT > 16 ? 1 : 2) void tile_kernel(const LinearArgs a, const unsigned tiles_n, const unsigned tiles_m)
+{
+    constexpr int CH = 32 * MT, RW = 32 * NT, SPS = MODE == kNarrow ? 2 : 1, SPQ = 4 / SPS, NL = RW / 32;
+    __shared__ __attribute__((aligned(16))) uint8_t lds_x[2][RW * 128];
+    __shared__ unsigned lds_s[BLOCKS ? 2 : 1][BLOCKS ? RW * 4 : 1];
+
+    // Workgroups go round the eight XCDs.  Each takes a run of tiles, in groups of four tiles of rows by all tiles of channels,
+    // so that what an XCD works on at one time shares weights and rows in its L2.
+    const unsigned total = tiles_n * tiles_m, per = (total + 7) / 8;
+    const unsigned id = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
+    if (id >= total) return;
+    const unsigned group = id / (4 * tiles_n), in_group = id - group * 4 * tiles_n;
+    const unsigned group_rows = min(4u, tiles_m - group * 4);
+    const unsigned tile_m = group * 4 + in_group % group_rows, tile_n = in_group / group_rows;
+
+    const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, r = lane & 15, g = lane >> 4;
+    const int wn = wave & 1, wm = wave >> 1;
+    const long long row0 = (long long)tile_m * RW;
+    const int rows = (int)min((long long)RW, a.rows - row0);
+    const int stride = a.blocks * (MODE == kNarrow ? 16 : 32);            // bytes of a row's codes
+    const __amdgpu_buffer_rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.x + row0 * stride), 0, rows * stride, 0x00020000);
+    const int x_row = t >> 3, x_piece = (t & 7) ^ (x_row & 7);
+    const int x_off = x_row * stride + x_piece * 16;
+    const int stages = (a.steps + SPS - 1) / SPS;
+
+    u4 xv[NL];
+    auto fetch_rows = [&](int stage) {
+        const int at = stage * 128 + x_piece * 16;
+        // past the row's codes: an offset past the buffer's end, which reads as zeros
+        const int off = at < stride && stage < stages ? x_off + stage * 128 : (int)0x80000000;
+#pragma unroll
+        for (int i = 0; i < NL; ++i)
+            xv[i] = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(xr, off < 0 ? off : off + i * 32 * stride, 0, 0));
+    };
+    auto keep_rows = [&](int buffer) {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) *(u4*)&lds_x[buffer][i * 4096 + t * 16] = xv[i];
+    };
+    // thread t < RW: scales of row t of quad q, as one word per group of lanes
+    u4 sv = {};
+    auto fetch_scales = [&](int q) {
+        if constexpr (BLOCKS) {
+            u4 d = {};
+            if (t < rows && q < a.quads) {
+                const uint8_t* const s = a.xs + (row0 + t) * a.blocks + q * 16;
+                if (q * 16 + 16 <= a.blocks) {
+                    d = ((const Any16*)s)->v;
+                } else {
+                    for (int i = 0; q * 16 + i < a.blocks; ++i) {
+                        const unsigned b = (unsigned)s[i] << 8 * (i & 3);
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) d[w] |= i >> 2 == w ? b : 0u;
+                    }
+                }
+            }
+            sv = d;
+        }
+    };
+    auto keep_scales = [&](int buffer) {
+        if constexpr (BLOCKS)
+            if (t < RW) {
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const unsigned sel = (unsigned)w | (unsigned)(w + 4) << 8;
+                    const unsigned lo = __builtin_amdgcn_perm(sv[1], sv[0], sel), hi = __builtin_amdgcn_perm(sv[3], sv[2], sel);
+                    lds_s[buffer][(t >> 4) * 64 + w * 16 + (t & 15)] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+                }
+            }
+    };
+
+    // the wave's tiles of weights: buffers that begin at the first of them, a scalar offset for tile and step
+    const int first = (int)tile_n * (CH / 16) + wn * MT, last = a.tile_rows - 1 - first;       // (last < 0: the wave has none, and repeats the layer's last)
+    const long long base = min(first, a.tile_rows - 1);
+    const auto buffer_at = [](const uint8_t* p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, 0x7FFFFFFF, 0x00020000); };
+    const __amdgpu_buffer_rsrc_t wr = buffer_at(a.w + base * a.steps * 1024), wsr = buffer_at(a.ws + base * a.quads * 256);
+    u4 w[MT], wnext[MT];
+    unsigned ws[MT], wsnext[MT];
+    auto fetch_weights = [&](u4 (&to)[MT], int step) {
+        const int at = min(step, a.steps - 1);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+            to[i] = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(wr, lane * 16, (max(min(i, last), 0) * a.steps + at) * 1024, 0));
+    };
+    auto fetch_weight_scales = [&](unsigned (&to)[MT], int q) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+            to[i] = __builtin_amdgcn_raw_buffer_load_b32(wsr, lane * 4, (max(min(i, last), 0) * a.quads + min(q, a.quads - 1)) * 256, 0);
+    };
+
+    f4 acc[MT][NT] = {};
+    fetch_rows(0);
+    fetch_scales(0);
+    fetch_weights(w, 0);
+    fetch_weight_scales(ws, 0);
+    keep_rows(0);
+    keep_scales(0);
+    fetch_rows(1);
+    for (int q = 0; q < a.quads; ++q) {
+        fetch_weight_scales(wsnext, q + 1);
+        fetch_scales(q + 1);
+        unsigned xs[NT];
+#pragma unroll
+        for (int st = 0; st < SPQ; ++st) {
+            const int stage = q * SPQ + st, buffer = stage & 1;
+            __syncthreads();
+            if (st == 0) {
+#pragma unroll
+                for (int j = 0; j < NT; ++j) xs[j] = BLOCKS ? lds_s[q & 1][(wm * NT + j) * 64 + lane] : 127u * 0x01010101u;
+            }
+            keep_rows(buffer ^ 1);
+            if (st == SPQ - 1) keep_scales((q + 1) & 1);
+            fetch_rows(stage + 2);
+#pragma unroll
+            for (int u = 0; u < SPS; ++u) {
+                const int s = st * SPS + u, step = q * 4 + s;
+                fetch_weights(wnext, step + 1);
+                const uint8_t* const x = &lds_x[buffer][(wm * NT * 16 + r) * 128];
+                auto piece = [&](int j, int c) { return *(const u4*)(x + j * 2048 + (c ^ (r & 7)) * 16); };
+                if constexpr (MODE == kWide8) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        u4 xc[NT];
+#pragma unroll
+                        for (int j = 0; j < NT; ++j) xc[j] = piece(j, 2 * g + h);
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            b8 B[NT];
+#pragma unroll
+                            for (int j = 0; j < NT; ++j) B[j] = wide8(xc[j][2 * k], xc[j][2 * k + 1], mx_scale(xs[j] >> 8 * s & 255u));
+#pragma unroll
+                            for (int i = 0; i < MT; ++i) {
+                                const b8 A = wide4(w[i][2 * h + k], mx_scale(ws[i] >> 8 * s & 255u));
+#pragma unroll
+                                for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, B[j], acc[i][j], 0, 0, 0);
+                            }
+                        }
+                    }
+                } else {
+                    i8v B[NT];
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) {
+                        const u4 lo = MODE == kNarrow ? piece(j, u * 4 + g) : piece(j, g), hi = MODE == kNarrow ? (u4){} : piece(j, 4 + g);
+                        B[j] = (i8v){(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+                    }
+#pragma unroll
+                    for (int i = 0; i < MT; ++i) {
+                        const i8v A = {(int)w[i].x, (int)w[i].y, (int)w[i].z, (int)w[i].w, 0, 0, 0, 0};
+#pragma unroll
+                        for (int j = 0; j < NT; ++j)
+                            acc[i][j] = scaled_mma<MODE == kNarrow ? 4 : 0>(A, B[j], acc[i][j], s, ws[i], xs[j]);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < MT; ++i) w[i] = wnext[i];
+                __builtin_amdgcn_sched_barrier(0);                        // (steps moved into each other spill)
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) ws[i] = wsnext[i];
+    }
+    constexpr int FMT = MODE == kNarrow ? SBN_MXFP4 : BLOCKS ? SBN_MXFP8 : SBN_FP8_ROW;
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+            finish4<FMT, T>(a, row0 + (wm * NT + j) * 16 + r, ((int)tile_n * (CH / 16) + wn * MT + i) * 16 + g * 4, acc[i][j]);
+}
+
+template <int FMT, class T, int MT, int NT>
+void launch_tiles(const LinearArgs& a, hipStream_t stream)
+{
+    constexpr int MODE = FMT == SBN_MXFP4 ? kNarrow : sizeof(T) == 4 ? kWide8 : kScaled8;
+    const unsigned tn = (unsigned)((a.c_out + 32 * MT - 1) / (32 * MT)), tm = (unsigned)((a.rows + 32 * NT - 1) / (32 * NT));
+    tile_kernel<MODE, FMT != SBN_FP8_ROW, T, MT, NT><<<(tn * tm + 7) / 8 * 8, 256, 0, stream>>>(a, tn, tm);
+}
+
 template <int FMT, class T>
 int run_linear(LinearArgs a, hipStream_t stream)
 {
@@ -199,8 +397,16 @@ int run_linear(LinearArgs a, hipStream_t stream)
         b.x = a.x + r0 * a.blocks * (FMT == SBN_MXFP4 ? 16 : 32);
         b.xs = a.xs + r0 * (FMT == SBN_FP8_ROW ? 4 : a.blocks);
         b.y = (T*)a.y + r0 * a.ldy;
+        int form = forced_kernel_form(SBN_LINEAR_MX);
+        if (!form) form = b.rows > 64 ? 88 : 1;
+        if ((long long)a.blocks * 32 * 256 >= 1ll << 31) form = 1;        // (a tile of rows has to lie within 31 bits)
         const dim3 grid((unsigned)a.tile_rows, (unsigned)((b.rows + 15) / 16));
-        rows_kernel<FMT, T, 1><<<grid, 256, 0, stream>>>(b);
+        if (form == 88)
+            launch_tiles<FMT, T, 8, 8>(b, stream);
+        else if (form == 44)
+            launch_tiles<FMT, T, 4, 4>(b, stream);
+        else
+            rows_kernel<FMT, T, 1><<<grid, 256, 0, stream>>>(b);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return fail(SBN_EHIP, "sbn_linear_mx: %s", hipGetErrorString(e));
     }
     return SBN_OK;
