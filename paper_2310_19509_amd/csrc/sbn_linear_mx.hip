@@ -201,21 +201,32 @@ __global__ __launch_bounds__(256) void rows_kernel(const LinearArgs a)
             if (tile0 + t < a.tile_rows) finish4<FMT, T>(a, row, (tile0 + t) * 16 + g * 4, acc[t] + sums[0][t][lane] + sums[1][t][lane] + sums[2][t][lane]);
 }
 
-// Tiles: CH = 32 MT output channels x RW = 32 NT rows to a workgroup of 2 x 2 waves, each 16 MT x 16 NT.
-//
-// Weights go from memory straight to registers (a tile of the layout is one 16-byte load per lane), one step of 128 input channels
-// ahead.  Rows go through LDS in stages of 128 bytes of codes (two steps of 4-bit codes, one of 8-bit ones), two buffers: while a
-// stage is multiplied, the next one moves from registers to LDS and the one after it from memory to registers, so one barrier a
-// stage is enough.  Sixteen-byte pieces of a row lie at piece ^ (row & 7), which spreads the reads of eight rows over all banks.
-// The last quad's steps past c_in multiply zeros: leaving the loop among them would cost registers for every sum.
-// Scales of rows are turned, four steps at a time, into words that hold a lane's bytes of four steps, as the weights' are.
-enum { kNarrow, kScaled8, kWide8 };         // 4-bit rows; 8-bit rows on scaled multiplies; 8-bit rows as bfloat16
-template <int MODE, bool BLOCKS, class T, int MT, int NT>
-__global__ __launch_bounds__(256, MT * NT > 16 ? 1 : 2) void tile_kernel(const LinearArgs a, const unsigned tiles_n, const unsigned tiles_m)
+// One 16-byte piece per lane from a buffer straight to LDS, lane l's at `lds` + 16 l.  In inline assembly because the compiler, which cannot tell
+// the two halves of a double buffer apart, would wait for these loads before every read of the other half.  They have no output
+// registers; the caller waits (vmcnt) before the barrier behind which the pieces are read.
+__device__ inline void load_to_lds(u4 buffer, unsigned offset, unsigned scalar_offset, unsigned lds)
 {
-    constexpr int CH = 32 * MT, RW = 32 * NT, SPS = MODE == kNarrow ? 2 : 1, SPQ = 4 / SPS, NL = RW / 32;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "s"(lds), "v"(offset), "s"(buffer), "s"(scalar_offset) : "memory", "m0");
+}
+__device__ inline unsigned uniform(unsigned v) { return (unsigned)__builtin_amdgcn_readfirstlane((int)v); }
+
+// Tiles: CH = 16 MT WN output channels x RW = 16 NT WM rows to a workgroup of WN x WM waves, each 16 MT x 16 NT.
+//
+// The sums step through the input channels in stages: 128 bytes of a row's codes, which is 256 channels (two steps of multiplies) of 4-bit codes and
+// 128 (one) of 8-bit ones.  Rows go from memory straight to LDS, into the half of a double buffer that is not being read; weights go straight
+// to registers (a tile of the layout is one 16-byte load per lane), as only the WM waves side by side want the same ones.  Everything for the
+// next stage is asked for at the top of a stage, and waited for at the next top: one wait and one barrier a stage.
+// Sixteen-byte pieces of a row lie at piece ^ (row & 7), which spreads the reads of eight rows over all banks.
+// Scales of rows are turned, four steps at a time, into words that hold a lane's bytes of four steps, as the weights' are.
+// The last four steps are whole: past c_in they multiply zeros (leaving the loop among them would cost registers for every sum).
+enum { kNarrow, kScaled8, kWide8 };         // 4-bit rows; 8-bit rows on scaled multiplies; 8-bit rows as bfloat16
+template <int MODE, bool BLOCKS, class T, int MT, int NT, int WN, int WM>
+__global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(const LinearArgs a, const unsigned tiles_n, const unsigned tiles_m)
+{
+    constexpr int THREADS = 64 * WN * WM, CH = 16 * MT * WN, RW = 16 * NT * WM, SPS = MODE == kNarrow ? 2 : 1, SPQ = 4 / SPS, NL = RW * 8 / THREADS;
+    static_assert(RW <= THREADS && NL >= 1, "a row's scales belong to one thread");
     __shared__ __attribute__((aligned(16))) uint8_t lds_x[2][RW * 128];
-    __shared__ unsigned lds_s[BLOCKS ? 2 : 1][BLOCKS ? RW * 4 : 1];
+    __shared__ unsigned lds_s[BLOCKS ? 2 : 1][BLOCKS ? THREADS * 4 : 1];  // (as many rows as threads: all of them write)
 
     // Workgroups go round the eight XCDs.  Each takes a run of tiles, in groups of four tiles of rows by all tiles of channels,
     // so that what an XCD works on at one time shares weights and rows in its L2.
@@ -226,59 +237,57 @@ __global__ __launch_bounds__(256, MT * NT > 16 ? 1 : 2) void tile_kernel(const L
     const unsigned group_rows = min(4u, tiles_m - group * 4);
     const unsigned tile_m = group * 4 + in_group % group_rows, tile_n = in_group / group_rows;
 
-    const int t = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(t >> 6), lane = t & 63, r = lane & 15, g = lane >> 4;
-    const int wn = wave & 1, wm = wave >> 1;
+    const int t = threadIdx.x, wave = (int)uniform(t >> 6), lane = t & 63, r = lane & 15, g = lane >> 4;
+    const int wn = wave % WN, wm = wave / WN;
     const long long row0 = (long long)tile_m * RW;
     const int rows = (int)min((long long)RW, a.rows - row0);
     const int stride = a.blocks * (MODE == kNarrow ? 16 : 32);            // bytes of a row's codes
-    const __amdgpu_buffer_rsrc_t xr = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(a.x + row0 * stride), 0, rows * stride, 0x00020000);
-    const int x_row = t >> 3, x_piece = (t & 7) ^ (x_row & 7);
-    const int x_off = x_row * stride + x_piece * 16;
-    const int stages = (a.steps + SPS - 1) / SPS;
 
-    u4 xv[NL];
+    // rows: lane l of load i of a wave has piece (l & 7) ^ (l >> 3) of row l >> 3 of the eight rows that are the wave's in load i
+    const uint8_t* const x0 = a.x + row0 * stride;
+    const u4 xr = {uniform((unsigned)(uintptr_t)x0), uniform((unsigned)((uintptr_t)x0 >> 32)), (unsigned)(rows * stride), 0x00020000u};
+    const int x_piece = (lane & 7) ^ (lane >> 3);
+    unsigned x_off[NL];
+#pragma unroll
+    for (int i = 0; i < NL; ++i) x_off[i] = (unsigned)(min(i * (THREADS / 8) + wave * 8 + (lane >> 3), rows - 1) * stride + x_piece * 16);
+    const unsigned lds_rows = uniform((unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&lds_x[0][0]) + wave * 1024;
     auto fetch_rows = [&](int stage) {
-        const int at = stage * 128 + x_piece * 16;
-        // past the row's codes: an offset past the buffer's end, which reads as zeros
-        const int off = at < stride && stage < stages ? x_off + stage * 128 : (int)0x80000000;
+        const bool in = stage * 128 + x_piece * 16 < stride;              // past the row's codes: past the buffer's end, where zeros are read
 #pragma unroll
         for (int i = 0; i < NL; ++i)
-            xv[i] = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(xr, off < 0 ? off : off + i * 32 * stride, 0, 0));
+            load_to_lds(xr, in ? x_off[i] : 0x80000000u, stage * 128, lds_rows + (stage & 1) * (RW * 128) + i * (THREADS * 16));
     };
-    auto keep_rows = [&](int buffer) {
-#pragma unroll
-        for (int i = 0; i < NL; ++i) *(u4*)&lds_x[buffer][i * 4096 + t * 16] = xv[i];
-    };
-    // thread t < RW: scales of row t of quad q, as one word per group of lanes
+
+    // thread t: scales of row t of quad q, as one word per group of lanes.  Without branches, which would cost registers for every
+    // sum: what lies past the array is not read (the load slides back and is shifted), what lies past the row is masked, and rows
+    // past the last only meet sums that are not stored.  One load of 16 bytes: four of 4, each with 64 rows' lines to look
+    // up, took 40 % of the cache's accesses.
+    const uint8_t* const xs0 = a.xs + row0 * a.blocks;
+    const int most = (int)min((a.rows - row0) * a.blocks, 0x7FFFFFFFll) - 16;
     u4 sv = {};
     auto fetch_scales = [&](int q) {
-        if constexpr (BLOCKS) {
-            u4 d = {};
-            if (t < rows && q < a.quads) {
-                const uint8_t* const s = a.xs + (row0 + t) * a.blocks + q * 16;
-                if (q * 16 + 16 <= a.blocks) {
-                    d = ((const Any16*)s)->v;
-                } else {
-                    for (int i = 0; q * 16 + i < a.blocks; ++i) {
-                        const unsigned b = (unsigned)s[i] << 8 * (i & 3);
-#pragma unroll
-                        for (int w = 0; w < 4; ++w) d[w] |= i >> 2 == w ? b : 0u;
-                    }
-                }
-            }
-            sv = d;
-        }
+        if constexpr (BLOCKS) sv = ((const Bytes16*)(xs0 + min(t * a.blocks + q * 16, most)))->v;
     };
-    auto keep_scales = [&](int buffer) {
-        if constexpr (BLOCKS)
-            if (t < RW) {
+    auto keep_scales = [&](int q) {
+        if constexpr (BLOCKS) {
+            const int left = a.blocks - q * 16;                           // blocks of the row in this quad and after
+            const int over = max(t * a.blocks + q * 16 - most, 0);        // bytes that the load slid back
+            const u4 d = over & 8 ? (u4){sv.z, sv.w, 0, 0} : sv;
+            const u4 e = over & 4 ? (u4){d.y, d.z, d.w, 0} : d;
+            u4 v;
 #pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    const unsigned sel = (unsigned)w | (unsigned)(w + 4) << 8;
-                    const unsigned lo = __builtin_amdgcn_perm(sv[1], sv[0], sel), hi = __builtin_amdgcn_perm(sv[3], sv[2], sel);
-                    lds_s[buffer][(t >> 4) * 64 + w * 16 + (t & 15)] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
-                }
+            for (int w = 0; w < 4; ++w) {
+                const unsigned lo = e[w], hi = w < 3 ? e[w + 1 & 3] : 0u;
+                const int n = left - w * 4;
+                v[w] = __builtin_amdgcn_alignbyte(hi, lo, (unsigned)over) & (n >= 4 ? ~0u : n <= 0 ? 0u : (1u << 8 * n) - 1u);
             }
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const unsigned sel = (unsigned)w | (unsigned)(w + 4) << 8;
+                const unsigned lo = __builtin_amdgcn_perm(v[1], v[0], sel), hi = __builtin_amdgcn_perm(v[3], v[2], sel);
+                lds_s[q & 1][(t >> 4) * 64 + w * 16 + (t & 15)] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+            }
+        }
     };
 
     // the wave's tiles of weights: buffers that begin at the first of them, a scalar offset for tile and step
@@ -286,105 +295,148 @@ __global__ __launch_bounds__(256, MT * NT > 16 ? 1 : 2) void tile_kernel(const L
     const long long base = min(first, a.tile_rows - 1);
     const auto buffer_at = [](const uint8_t* p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, 0x7FFFFFFF, 0x00020000); };
     const __amdgpu_buffer_rsrc_t wr = buffer_at(a.w + base * a.steps * 1024), wsr = buffer_at(a.ws + base * a.quads * 256);
-    u4 w[MT], wnext[MT];
-    unsigned ws[MT], wsnext[MT];
     auto fetch_weights = [&](u4 (&to)[MT], int step) {
         const int at = min(step, a.steps - 1);
 #pragma unroll
         for (int i = 0; i < MT; ++i)
             to[i] = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(wr, lane * 16, (max(min(i, last), 0) * a.steps + at) * 1024, 0));
     };
+    unsigned ws[MT];
     auto fetch_weight_scales = [&](unsigned (&to)[MT], int q) {
 #pragma unroll
         for (int i = 0; i < MT; ++i)
             to[i] = __builtin_amdgcn_raw_buffer_load_b32(wsr, lane * 4, (max(min(i, last), 0) * a.quads + min(q, a.quads - 1)) * 256, 0);
     };
+    auto landed = [&] {
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0x0070);                               // vmcnt(0) lgkmcnt(0)
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
 
     f4 acc[MT][NT] = {};
-    fetch_rows(0);
+    // one step of 128 channels: s is its place in the quad, u in the stage
+    auto multiply = [&](const u4 (&w)[MT], const unsigned (&xs)[NT], int buffer, int s, int u) {
+        const uint8_t* const x = &lds_x[buffer][(wm * NT * 16 + r) * 128];
+        if constexpr (MODE == kWide8) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                b8 B[NT];
+#pragma unroll
+                for (int j = 0; j < NT; ++j) {
+                    const u2 c = *(const u2*)(x + j * 2048 + ((2 * g + k / 2) ^ (r & 7)) * 16 + k % 2 * 8);
+                    B[j] = wide8(c.x, c.y, mx_scale(xs[j] >> 8 * s & 255u));
+                }
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    const b8 A = wide4(w[i][k], mx_scale(ws[i] >> 8 * s & 255u));
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, B[j], acc[i][j], 0, 0, 0);
+                }
+            }
+        } else {
+            auto piece = [&](int j, int c) { return *(const u4*)(x + j * 2048 + (c ^ (r & 7)) * 16); };
+            constexpr int NB = NT < 4 ? NT : 4;                           // row tiles at a time
+#pragma unroll
+            for (int j0 = 0; j0 < NT; j0 += NB) {
+                i8v B[NB];
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    const u4 lo = MODE == kNarrow ? piece(j0 + j, u * 4 + g) : piece(j0 + j, g), hi = MODE == kNarrow ? (u4){} : piece(j0 + j, 4 + g);
+                    B[j] = (i8v){(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+                }
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    const i8v A = {(int)w[i].x, (int)w[i].y, (int)w[i].z, (int)w[i].w, 0, 0, 0, 0};
+#pragma unroll
+                    for (int j = 0; j < NB; ++j) acc[i][j0 + j] = scaled_mma<MODE == kNarrow ? 4 : 0>(A, B[j], acc[i][j0 + j], s, ws[i], xs[j0 + j]);
+                }
+            }
+        }
+    };
+
+    // weights of the current step, of the next one, and, where a stage has two steps, of the one after that
+    u4 w[MT], w1[MT];
     fetch_scales(0);
+    fetch_rows(0);
     fetch_weights(w, 0);
+    if constexpr (SPS == 2) fetch_weights(w1, 1);
     fetch_weight_scales(ws, 0);
-    keep_rows(0);
     keep_scales(0);
-    fetch_rows(1);
     for (int q = 0; q < a.quads; ++q) {
-        fetch_weight_scales(wsnext, q + 1);
-        fetch_scales(q + 1);
-        unsigned xs[NT];
+        unsigned wsnext[MT], xs[NT];
 #pragma unroll
         for (int st = 0; st < SPQ; ++st) {
-            const int stage = q * SPQ + st, buffer = stage & 1;
-            __syncthreads();
+            const int stage = q * SPQ + st, buffer = st & 1;
+            landed();
+            if (st == 0) {
+                fetch_weight_scales(wsnext, q + 1);
+                fetch_scales(q + 1);
+            }
+            fetch_rows(stage + 1);                                        // (past the last stage: zeros, into the half that nothing reads any more)
+            u4 w2[MT];
+            fetch_weights(w2, (stage + 1) * SPS);
+            __builtin_amdgcn_sched_barrier(0);
             if (st == 0) {
 #pragma unroll
                 for (int j = 0; j < NT; ++j) xs[j] = BLOCKS ? lds_s[q & 1][(wm * NT + j) * 64 + lane] : 127u * 0x01010101u;
             }
-            keep_rows(buffer ^ 1);
-            if (st == SPQ - 1) keep_scales((q + 1) & 1);
-            fetch_rows(stage + 2);
+            if (st == SPQ - 1) keep_scales(q + 1);
+            multiply(w, xs, buffer, st * SPS, 0);
+            if constexpr (SPS == 2) {
+                __builtin_amdgcn_sched_barrier(0);
+                fetch_weights(w, (stage + 1) * SPS + 1);
+                __builtin_amdgcn_sched_barrier(0);
+                multiply(w1, xs, buffer, st * SPS + 1, 1);
 #pragma unroll
-            for (int u = 0; u < SPS; ++u) {
-                const int s = st * SPS + u, step = q * 4 + s;
-                fetch_weights(wnext, step + 1);
-                const uint8_t* const x = &lds_x[buffer][(wm * NT * 16 + r) * 128];
-                auto piece = [&](int j, int c) { return *(const u4*)(x + j * 2048 + (c ^ (r & 7)) * 16); };
-                if constexpr (MODE == kWide8) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        u4 xc[NT];
-#pragma unroll
-                        for (int j = 0; j < NT; ++j) xc[j] = piece(j, 2 * g + h);
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            b8 B[NT];
-#pragma unroll
-                            for (int j = 0; j < NT; ++j) B[j] = wide8(xc[j][2 * k], xc[j][2 * k + 1], mx_scale(xs[j] >> 8 * s & 255u));
-#pragma unroll
-                            for (int i = 0; i < MT; ++i) {
-                                const b8 A = wide4(w[i][2 * h + k], mx_scale(ws[i] >> 8 * s & 255u));
-#pragma unroll
-                                for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, B[j], acc[i][j], 0, 0, 0);
-                            }
-                        }
-                    }
-                } else {
-                    i8v B[NT];
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) {
-                        const u4 lo = MODE == kNarrow ? piece(j, u * 4 + g) : piece(j, g), hi = MODE == kNarrow ? (u4){} : piece(j, 4 + g);
-                        B[j] = (i8v){(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
-                    }
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        const i8v A = {(int)w[i].x, (int)w[i].y, (int)w[i].z, (int)w[i].w, 0, 0, 0, 0};
-#pragma unroll
-                        for (int j = 0; j < NT; ++j)
-                            acc[i][j] = scaled_mma<MODE == kNarrow ? 4 : 0>(A, B[j], acc[i][j], s, ws[i], xs[j]);
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < MT; ++i) w[i] = wnext[i];
-                __builtin_amdgcn_sched_barrier(0);                        // (steps moved into each other spill)
+                for (int i = 0; i < MT; ++i) w1[i] = w[i];
             }
+#pragma unroll
+            for (int i = 0; i < MT; ++i) w[i] = w2[i];
         }
 #pragma unroll
         for (int i = 0; i < MT; ++i) ws[i] = wsnext[i];
     }
+    landed();                                                             // nothing may be on its way to LDS when the workgroup ends
+
     constexpr int FMT = MODE == kNarrow ? SBN_MXFP4 : BLOCKS ? SBN_MXFP8 : SBN_FP8_ROW;
+    const int n0 = first * 16 + g * 4;
+    f4 bias[MT];
 #pragma unroll
-    for (int j = 0; j < NT; ++j)
+    for (int i = 0; i < MT; ++i) bias[i] = *(const f4*)(a.bias + min(n0 + i * 16, a.tile_rows * 16 - 4));
+    float row_scale[NT];
+    if constexpr (FMT == SBN_FP8_ROW)
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
-            finish4<FMT, T>(a, row0 + (wm * NT + j) * 16 + r, ((int)tile_n * (CH / 16) + wn * MT + i) * 16 + g * 4, acc[i][j]);
+        for (int j = 0; j < NT; ++j) row_scale[j] = ((const float*)a.xs)[row0 + min((wm * NT + j) * 16 + r, rows - 1)];
+    const bool relu = a.act == SBN_ACT_RELU, whole = rows == RW && (int)(tile_n + 1) * CH <= a.c_out;
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        const int row = (wm * NT + j) * 16 + r;
+        T* const y = (T*)a.y + (row0 + row) * a.ldy + n0;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            f4 v = acc[i][j];
+            if constexpr (FMT == SBN_FP8_ROW) v *= row_scale[j];
+            v += bias[i];
+            if (relu)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) v[c] = v[c] > 0.0f ? v[c] : 0.0f;
+            if (whole)
+                put4(y + i * 16, 4, v);
+            else if (row < rows && n0 + i * 16 < a.c_out)
+                put4(y + i * 16, a.c_out - n0 - i * 16, v);
+        }
+    }
 }
 
-template <int FMT, class T, int MT, int NT>
+template <int FMT, class T, int MT, int NT, int WN, int WM>
 void launch_tiles(const LinearArgs& a, hipStream_t stream)
 {
     constexpr int MODE = FMT == SBN_MXFP4 ? kNarrow : sizeof(T) == 4 ? kWide8 : kScaled8;
-    const unsigned tn = (unsigned)((a.c_out + 32 * MT - 1) / (32 * MT)), tm = (unsigned)((a.rows + 32 * NT - 1) / (32 * NT));
-    tile_kernel<MODE, FMT != SBN_FP8_ROW, T, MT, NT><<<(tn * tm + 7) / 8 * 8, 256, 0, stream>>>(a, tn, tm);
+    constexpr int CH = 16 * MT * WN, RW = 16 * NT * WM;
+    const unsigned tn = (unsigned)((a.c_out + CH - 1) / CH), tm = (unsigned)((a.rows + RW - 1) / RW);
+    tile_kernel<MODE, FMT != SBN_FP8_ROW, T, MT, NT, WN, WM><<<(tn * tm + 7) / 8 * 8, 64 * WN * WM, 0, stream>>>(a, tn, tm);
 }
 
 template <int FMT, class T>
@@ -399,12 +451,14 @@ int run_linear(LinearArgs a, hipStream_t stream)
         b.y = (T*)a.y + r0 * a.ldy;
         int form = forced_kernel_form(SBN_LINEAR_MX);
         if (!form) form = b.rows > 64 ? 88 : 1;
-        if ((long long)a.blocks * 32 * 256 >= 1ll << 31) form = 1;        // (a tile of rows has to lie within 31 bits)
+        if ((long long)a.blocks * 32 * 256 >= 1ll << 31 || b.rows * a.blocks < 16) form = 1;      // (a tile of rows has to lie within 31 bits, the scales to fill a load)
         const dim3 grid((unsigned)a.tile_rows, (unsigned)((b.rows + 15) / 16));
         if (form == 88)
-            launch_tiles<FMT, T, 8, 8>(b, stream);
+            launch_tiles<FMT, T, 4, 8, 4, 2>(b, stream);
+        else if (form == 48)
+            launch_tiles<FMT, T, 4, 8, 2, 2>(b, stream);
         else if (form == 44)
-            launch_tiles<FMT, T, 4, 4>(b, stream);
+            launch_tiles<FMT, T, 4, 4, 2, 2>(b, stream);
         else
             rows_kernel<FMT, T, 1><<<grid, 256, 0, stream>>>(b);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return fail(SBN_EHIP, "sbn_linear_mx: %s", hipGetErrorString(e));

@@ -26,6 +26,7 @@ typedef short s2 __attribute__((ext_vector_type(2)));
 // accesses there, so one form of load serves all strides.
 struct __attribute__((packed, aligned(2))) Any16 { u4 v; };
 struct __attribute__((packed, aligned(2))) Any8 { u2 v; };
+struct __attribute__((packed, aligned(1))) Bytes16 { u4 v; };
 
 template <class T> struct Elem;
 template <> struct Elem<float> {

@@ -73,6 +73,24 @@ def test_against_64_bits(fmt, dtype, rows, k, n, bias, act):
     assert torch.equal(y, _run(p, codes, scales, fmt, rows, dtype))       # the same bits each time
 
 
+@pytest.mark.parametrize("form", [1, 44, 48, 88])
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,k,n,bias,act", [(1, 32, 1, False, 0), (5, 96, 40, True, 1), (129, 130, 145, True, 0), (255, 1025, 700, False, 1), (257, 544, 260, True, 0), (300, 4100, 64, False, 0)])
+def test_every_form(form, fmt, dtype, rows, k, n, bias, act):
+    p, w, b = _layer(rows + k + n, n, k, bias, act)
+    codes, scales = _rows(rows * k + 1, rows, k, fmt)
+    x = L.values(codes.cpu().numpy(), scales.cpu().numpy(), fmt, k)
+    S.sbn_force_kernel_form(S.SBN_LINEAR_MX, form)
+    try:
+        y = _run(p, codes, scales, fmt, rows, dtype, pad=n % 2)
+        again = _run(p, codes, scales, fmt, rows, dtype)
+    finally:
+        S.sbn_force_kernel_form(S.SBN_LINEAR_MX, 0)
+    _check(y, x, w, b, act, fmt, dtype)
+    assert torch.equal(y, again)
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("rows", [1, 40, 300])
 def test_every_weight_counts_where_it_lies(fmt, rows):
