@@ -221,7 +221,7 @@ __device__ inline unsigned uniform(unsigned v) { return (unsigned)__builtin_amdg
 // The last four steps are whole: past c_in they multiply zeros (leaving the loop among them would cost registers for every sum).
 enum { kNarrow, kScaled8, kWide8 };         // 4-bit rows; 8-bit rows on scaled multiplies; 8-bit rows as bfloat16
 template <int MODE, bool BLOCKS, class T, int MT, int NT, int WN, int WM>
-__global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(const LinearArgs a, const unsigned tiles_n, const unsigned tiles_m)
+__global__ __launch_bounds__(64 * WN * WM, MT * NT > 32 ? 1 : 2) void tile_kernel(const LinearArgs a, const unsigned tiles_n, const unsigned tiles_m)
 {
     constexpr int THREADS = 64 * WN * WM, CH = 16 * MT * WN, RW = 16 * NT * WM, SPS = MODE == kNarrow ? 2 : 1, SPQ = 4 / SPS, NL = RW * 8 / THREADS;
     static_assert(RW <= THREADS && NL >= 1, "a row's scales belong to one thread");
@@ -316,43 +316,46 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(const LinearArgs 
     };
 
     f4 acc[MT][NT] = {};
-    // one step of 128 channels: s is its place in the quad, u in the stage
-    auto multiply = [&](const u4 (&w)[MT], const unsigned (&xs)[NT], int buffer, int s, int u) {
-        const uint8_t* const x = &lds_x[buffer][(wm * NT * 16 + r) * 128];
-        if constexpr (MODE == kWide8) {
+    const uint8_t* const x_lane = &lds_x[0][(wm * NT * 16 + r) * 128];
+    // one step of 128 channels in bfloat16; s is its place in the quad
+    auto multiply_wide = [&](const u4 (&w)[MT], const unsigned (&xs)[NT], int buffer, int s) {
+        const uint8_t* const x = x_lane + buffer * (RW * 128);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                b8 B[NT];
+        for (int k = 0; k < 4; ++k) {
+            b8 B[NT];
 #pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    const u2 c = *(const u2*)(x + j * 2048 + ((2 * g + k / 2) ^ (r & 7)) * 16 + k % 2 * 8);
-                    B[j] = wide8(c.x, c.y, mx_scale(xs[j] >> 8 * s & 255u));
-                }
-#pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    const b8 A = wide4(w[i][k], mx_scale(ws[i] >> 8 * s & 255u));
-#pragma unroll
-                    for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, B[j], acc[i][j], 0, 0, 0);
-                }
+            for (int j = 0; j < NT; ++j) {
+                const u2 c = *(const u2*)(x + j * 2048 + ((2 * g + k / 2) ^ (r & 7)) * 16 + k % 2 * 8);
+                B[j] = wide8(c.x, c.y, mx_scale(xs[j] >> 8 * s & 255u));
             }
-        } else {
-            auto piece = [&](int j, int c) { return *(const u4*)(x + j * 2048 + (c ^ (r & 7)) * 16); };
-            constexpr int NB = NT < 4 ? NT : 4;                           // row tiles at a time
 #pragma unroll
-            for (int j0 = 0; j0 < NT; j0 += NB) {
-                i8v B[NB];
+            for (int i = 0; i < MT; ++i) {
+                const b8 A = wide4(w[i][k], mx_scale(ws[i] >> 8 * s & 255u));
 #pragma unroll
-                for (int j = 0; j < NB; ++j) {
-                    const u4 lo = MODE == kNarrow ? piece(j0 + j, u * 4 + g) : piece(j0 + j, g), hi = MODE == kNarrow ? (u4){} : piece(j0 + j, 4 + g);
-                    B[j] = (i8v){(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
-                }
-#pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    const i8v A = {(int)w[i].x, (int)w[i].y, (int)w[i].z, (int)w[i].w, 0, 0, 0, 0};
-#pragma unroll
-                    for (int j = 0; j < NB; ++j) acc[i][j0 + j] = scaled_mma<MODE == kNarrow ? 4 : 0>(A, B[j], acc[i][j0 + j], s, ws[i], xs[j0 + j]);
-                }
+                for (int j = 0; j < NT; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, B[j], acc[i][j], 0, 0, 0);
             }
+        }
+    };
+    // The scaled multiplies take a stage in chunks of NB row tiles, a chunk's rows read from LDS while the one before it is multiplied.
+    constexpr int NB = MODE == kNarrow ? (NT < 4 ? NT : 4) : 2, CHUNKS = SPS * NT / NB;
+    i8v B[2][NB];
+    auto read_chunk = [&](int c, int buffer) {
+        const int u = c / (NT / NB), j0 = c % (NT / NB) * NB;
+        const uint8_t* const x = x_lane + buffer * (RW * 128);
+        auto piece = [&](int j, int p) { return *(const u4*)(x + j * 2048 + (p ^ (r & 7)) * 16); };
+#pragma unroll
+        for (int j = 0; j < NB; ++j) {
+            const u4 lo = MODE == kNarrow ? piece(j0 + j, u * 4 + g) : piece(j0 + j, g), hi = MODE == kNarrow ? (u4){} : piece(j0 + j, 4 + g);
+            B[c & 1][j] = (i8v){(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+        }
+    };
+    auto multiply_chunk = [&](int c, const u4 (&w)[MT], const unsigned (&xs)[NT], int s) {
+        const int j0 = c % (NT / NB) * NB;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+            const i8v A = {(int)w[i].x, (int)w[i].y, (int)w[i].z, (int)w[i].w, 0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < NB; ++j) acc[i][j0 + j] = scaled_mma<MODE == kNarrow ? 4 : 0>(A, B[c & 1][j], acc[i][j0 + j], s, ws[i], xs[j0 + j]);
         }
     };
 
@@ -370,7 +373,10 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(const LinearArgs 
         for (int st = 0; st < SPQ; ++st) {
             const int stage = q * SPQ + st, buffer = st & 1;
             landed();
+            if constexpr (MODE != kWide8) read_chunk(0, buffer);
             if (st == 0) {
+#pragma unroll
+                for (int j = 0; j < NT; ++j) xs[j] = BLOCKS ? lds_s[q & 1][(wm * NT + j) * 64 + lane] : 127u * 0x01010101u;
                 fetch_weight_scales(wsnext, q + 1);
                 fetch_scales(q + 1);
             }
@@ -378,19 +384,22 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(const LinearArgs 
             u4 w2[MT];
             fetch_weights(w2, (stage + 1) * SPS);
             __builtin_amdgcn_sched_barrier(0);
-            if (st == 0) {
+            if constexpr (MODE == kWide8) {
+                if (st == SPQ - 1) keep_scales(q + 1);
+                multiply_wide(w, xs, buffer, st);
+            } else {
 #pragma unroll
-                for (int j = 0; j < NT; ++j) xs[j] = BLOCKS ? lds_s[q & 1][(wm * NT + j) * 64 + lane] : 127u * 0x01010101u;
-            }
-            if (st == SPQ - 1) keep_scales(q + 1);
-            multiply(w, xs, buffer, st * SPS, 0);
-            if constexpr (SPS == 2) {
-                __builtin_amdgcn_sched_barrier(0);
-                fetch_weights(w, (stage + 1) * SPS + 1);
-                __builtin_amdgcn_sched_barrier(0);
-                multiply(w1, xs, buffer, st * SPS + 1, 1);
+                for (int c = 0; c < CHUNKS; ++c) {
+                    if (c + 1 < CHUNKS) read_chunk(c + 1, buffer);
+                    if (SPS == 2 && c == CHUNKS / 2) fetch_weights(w, (stage + 1) * SPS + 1);       // (the first step's registers are free now)
+                    __builtin_amdgcn_sched_barrier(0);
+                    multiply_chunk(c, c < CHUNKS / SPS ? w : w1, xs, st * SPS + c / (CHUNKS / SPS));
+                    if (st == SPQ - 1 && c == 0) keep_scales(q + 1);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if constexpr (SPS == 2)
 #pragma unroll
-                for (int i = 0; i < MT; ++i) w1[i] = w[i];
+                    for (int i = 0; i < MT; ++i) w1[i] = w[i];
             }
 #pragma unroll
             for (int i = 0; i < MT; ++i) w[i] = w2[i];
@@ -455,6 +464,8 @@ int run_linear(LinearArgs a, hipStream_t stream)
         const dim3 grid((unsigned)a.tile_rows, (unsigned)((b.rows + 15) / 16));
         if (form == 88)
             launch_tiles<FMT, T, 4, 8, 4, 2>(b, stream);
+        else if (form == 164)
+            launch_tiles<FMT, T, 4, 16, 4, 1>(b, stream);
         else if (form == 48)
             launch_tiles<FMT, T, 4, 8, 2, 2>(b, stream);
         else if (form == 44)
