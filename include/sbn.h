@@ -339,7 +339,7 @@ int sbn_conv3x3_sparse(const sbn_packed_t* p, const float* x, float* y,
  * and at least 4 high, the automatic choice otherwise; 3004, 3008, 3016: the few-pixel
  * kernel with 4, 8 or 16 waves, any stride).  Layers whose shape leaves no other choice (c_in <= 64,
  * c_in not a multiple of 4, stride 2) ignore all but the few-pixel forms.  SBN_LINEAR_MX (sbn_linear_mx): 1: 16 rows per
- * workgroup; 44, 88: tiles of 128 x 128 and 256 x 256.  Unknown values: SBN_EINVAL.
+ * workgroup; 44, 88, 164: tiles of 128 x 128, and of 256 x 256 to eight or four waves.  Unknown values: SBN_EINVAL.
  * Not synchronised with launches in flight on other threads.
  */
 int sbn_force_kernel_form(int kind, int form);

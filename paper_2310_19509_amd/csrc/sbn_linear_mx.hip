@@ -102,6 +102,13 @@ __device__ inline f4 scaled_mma(i8v a, i8v b, f4 c, int s, unsigned sa, unsigned
     }
 }
 
+// Four values in 16 bits each.
+template <class T>
+__device__ inline u2 packed(f4 v)
+{
+    const T t[4] = {Elem<T>::put(v[0]), Elem<T>::put(v[1]), Elem<T>::put(v[2]), Elem<T>::put(v[3])};
+    return __builtin_bit_cast(u2, t);
+}
 // Four consecutive output channels of a row.
 template <class T>
 __device__ inline void put4(T* y, int n, f4 v)
@@ -110,8 +117,7 @@ __device__ inline void put4(T* y, int n, f4 v)
         if constexpr (sizeof(T) == 4) {
             ((Any16*)y)->v = __builtin_bit_cast(u4, v);
         } else {
-            T t[4] = {Elem<T>::put(v[0]), Elem<T>::put(v[1]), Elem<T>::put(v[2]), Elem<T>::put(v[3])};
-            ((Any8*)y)->v = __builtin_bit_cast(u2, t);
+            ((Any8*)y)->v = packed<T>(v);
         }
     } else {
 #pragma unroll
@@ -212,10 +218,10 @@ __device__ inline unsigned uniform(unsigned v) { return (unsigned)__builtin_amdg
 
 // Tiles: CH = 16 MT WN output channels x RW = 16 NT WM rows to a workgroup of WN x WM waves, each 16 MT x 16 NT.
 //
-// The sums step through the input channels in stages: 128 bytes of a row's codes, which is 256 channels (two steps of multiplies) of 4-bit codes and
-// 128 (one) of 8-bit ones.  Rows go from memory straight to LDS, into the half of a double buffer that is not being read; weights go straight
-// to registers (a tile of the layout is one 16-byte load per lane), as only the WM waves side by side want the same ones.  Everything for the
-// next stage is asked for at the top of a stage, and waited for at the next top: one wait and one barrier a stage.
+// The sums step through the input channels in stages: 256 bytes of a row's codes, which is 512 channels (four steps of multiplies) of 4-bit codes,
+// 128 bytes (one step, twice as long) of 8-bit ones.  Rows go from memory straight to LDS, into the half of a double buffer that is not being read; weights go straight
+// to registers (a tile of the layout is one 16-byte load per lane), as only the WM waves side by side want the same ones.  One wait and one barrier
+// a stage, at its top.
 // Sixteen-byte pieces of a row lie at piece ^ (row & 7), which spreads the reads of eight rows over all banks.
 // Scales of rows are turned, four steps at a time, into words that hold a lane's bytes of four steps, as the weights' are.
 // The last four steps are whole: past c_in they multiply zeros (leaving the loop among them would cost registers for every sum).
@@ -223,9 +229,10 @@ enum { kNarrow, kScaled8, kWide8 };         // 4-bit rows; 8-bit rows on scaled 
 template <int MODE, bool BLOCKS, class T, int MT, int NT, int WN, int WM>
 __global__ __launch_bounds__(64 * WN * WM, MT * NT > 32 ? 1 : 2) void tile_kernel(const LinearArgs a, const unsigned tiles_n, const unsigned tiles_m)
 {
-    constexpr int THREADS = 64 * WN * WM, CH = 16 * MT * WN, RW = 16 * NT * WM, SPS = MODE == kNarrow ? 2 : 1, SPQ = 4 / SPS, NL = RW * 8 / THREADS;
+    constexpr int THREADS = 64 * WN * WM, CH = 16 * MT * WN, RW = 16 * NT * WM, SB = MODE == kNarrow ? 256 : 128, SPS = MODE == kNarrow ? 4 : 1, SPQ = 4 / SPS;
+    constexpr int PIECES = SB / 16, NL = RW * PIECES / THREADS;            // pieces of a row's stage, loads of a wave for it
     static_assert(RW <= THREADS && NL >= 1, "a row's scales belong to one thread");
-    __shared__ __attribute__((aligned(16))) uint8_t lds_x[2][RW * 128];
+    __shared__ __attribute__((aligned(16))) uint8_t lds_x[2][RW * SB];
     __shared__ unsigned lds_s[BLOCKS ? 2 : 1][BLOCKS ? THREADS * 4 : 1];  // (as many rows as threads: all of them write)
 
     // Workgroups go round the eight XCDs.  Each takes a run of tiles, in groups of four tiles of rows by all tiles of channels,
@@ -243,19 +250,17 @@ __global__ __launch_bounds__(64 * WN * WM, MT * NT > 32 ? 1 : 2) void tile_kerne
     const int rows = (int)min((long long)RW, a.rows - row0);
     const int stride = a.blocks * (MODE == kNarrow ? 16 : 32);            // bytes of a row's codes
 
-    // rows: lane l of load i of a wave has piece (l & 7) ^ (l >> 3) of row l >> 3 of the eight rows that are the wave's in load i
+    // rows: a load of a wave is 64 / PIECES rows; lane l has piece (l % PIECES) ^ (row & 7) of row l / PIECES of them
     const uint8_t* const x0 = a.x + row0 * stride;
     const u4 xr = {uniform((unsigned)(uintptr_t)x0), uniform((unsigned)((uintptr_t)x0 >> 32)), (unsigned)(rows * stride), 0x00020000u};
-    const int x_piece = (lane & 7) ^ (lane >> 3);
-    unsigned x_off[NL];
+    const int x_row = wave * (64 / PIECES) + lane / PIECES, x_piece = lane % PIECES ^ (x_row & 7);
+    const unsigned x_off = (unsigned)(x_row * stride + x_piece * 16), lds_rows = uniform((unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&lds_x[0][0]) + wave * 1024;
+    auto fetch_rows = [&](int stage, int from, int to) {
+        // past the row's codes, and past the last row: past the buffer's end, where zeros are read
+        const unsigned off = stage * SB + x_piece * 16 < stride ? x_off : 0x80000000u;
 #pragma unroll
-    for (int i = 0; i < NL; ++i) x_off[i] = (unsigned)(min(i * (THREADS / 8) + wave * 8 + (lane >> 3), rows - 1) * stride + x_piece * 16);
-    const unsigned lds_rows = uniform((unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&lds_x[0][0]) + wave * 1024;
-    auto fetch_rows = [&](int stage) {
-        const bool in = stage * 128 + x_piece * 16 < stride;              // past the row's codes: past the buffer's end, where zeros are read
-#pragma unroll
-        for (int i = 0; i < NL; ++i)
-            load_to_lds(xr, in ? x_off[i] : 0x80000000u, stage * 128, lds_rows + (stage & 1) * (RW * 128) + i * (THREADS * 16));
+        for (int i = from; i < to; ++i)
+            load_to_lds(xr, off + (unsigned)(i * (THREADS / PIECES) * stride), stage * SB, lds_rows + (stage & 1) * (RW * SB) + i * (THREADS * 16));
     };
 
     // thread t: scales of row t of quad q, as one word per group of lanes.  Without branches, which would cost registers for every
@@ -316,16 +321,17 @@ __global__ __launch_bounds__(64 * WN * WM, MT * NT > 32 ? 1 : 2) void tile_kerne
     };
 
     f4 acc[MT][NT] = {};
-    const uint8_t* const x_lane = &lds_x[0][(wm * NT * 16 + r) * 128];
-    // one step of 128 channels in bfloat16; s is its place in the quad
-    auto multiply_wide = [&](const u4 (&w)[MT], const unsigned (&xs)[NT], int buffer, int s) {
-        const uint8_t* const x = x_lane + buffer * (RW * 128);
+    const uint8_t* const x_lane = &lds_x[0][(wm * NT * 16 + r) * SB];
+    const int piece0 = (g ^ (r & 7)) * 16, piece1 = piece0 ^ 64;           // where pieces g and 4 + g of the lane's row lie
+    // one step of 128 channels in bfloat16; u is its place in the stage, s in the quad
+    auto multiply_wide = [&](const u4 (&w)[MT], const unsigned (&xs)[NT], int buffer, int u, int s) {
+        const uint8_t* const x = x_lane + buffer * (RW * SB);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             b8 B[NT];
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                const u2 c = *(const u2*)(x + j * 2048 + ((2 * g + k / 2) ^ (r & 7)) * 16 + k % 2 * 8);
+                const u2 c = *(const u2*)(x + j * (16 * SB) + u * 128 + ((2 * g + k / 2) ^ (r & 7)) * 16 + k % 2 * 8);
                 B[j] = wide8(c.x, c.y, mx_scale(xs[j] >> 8 * s & 255u));
             }
 #pragma unroll
@@ -337,20 +343,20 @@ __global__ __launch_bounds__(64 * WN * WM, MT * NT > 32 ? 1 : 2) void tile_kerne
         }
     };
     // The scaled multiplies take a stage in chunks of NB row tiles, a chunk's rows read from LDS while the one before it is multiplied.
-    constexpr int NB = MODE == kNarrow ? (NT < 4 ? NT : 4) : 2, CHUNKS = SPS * NT / NB;
+    constexpr int NB = MODE == kNarrow ? (NT < 4 ? NT : 4) : 2, CPS = NT / NB;          // chunks of a step
     i8v B[2][NB];
     auto read_chunk = [&](int c, int buffer) {
-        const int u = c / (NT / NB), j0 = c % (NT / NB) * NB;
-        const uint8_t* const x = x_lane + buffer * (RW * 128);
-        auto piece = [&](int j, int p) { return *(const u4*)(x + j * 2048 + (p ^ (r & 7)) * 16); };
+        const int u = c / CPS, j0 = c % CPS * NB;
+        const uint8_t* const x = x_lane + buffer * (RW * SB);
+        auto piece = [&](int j, int p) { return *(const u4*)(x + j * (16 * SB) + p / 8 * 128 + (p / 4 % 2 ? piece1 : piece0)); };          // (p without g)
 #pragma unroll
         for (int j = 0; j < NB; ++j) {
-            const u4 lo = MODE == kNarrow ? piece(j0 + j, u * 4 + g) : piece(j0 + j, g), hi = MODE == kNarrow ? (u4){} : piece(j0 + j, 4 + g);
+            const u4 lo = MODE == kNarrow ? piece(j0 + j, u * 4) : piece(j0 + j, u * 8), hi = MODE == kNarrow ? (u4){} : piece(j0 + j, u * 8 + 4);
             B[c & 1][j] = (i8v){(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
         }
     };
     auto multiply_chunk = [&](int c, const u4 (&w)[MT], const unsigned (&xs)[NT], int s) {
-        const int j0 = c % (NT / NB) * NB;
+        const int j0 = c % CPS * NB;
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const i8v A = {(int)w[i].x, (int)w[i].y, (int)w[i].z, (int)w[i].w, 0, 0, 0, 0};
@@ -359,19 +365,20 @@ __global__ __launch_bounds__(64 * WN * WM, MT * NT > 32 ? 1 : 2) void tile_kerne
         }
     };
 
-    // weights of the current step, of the next one, and, where a stage has two steps, of the one after that
-    u4 w[MT], w1[MT];
+    // Weights are asked for two steps ahead (8-bit rows: one, their steps are twice as long); the rows of the next stage during this one's first step.
+    constexpr int SETS = MODE == kNarrow ? 3 : 2, AHEAD = SETS - 1;
+    u4 w[SETS][MT];
     fetch_scales(0);
-    fetch_rows(0);
-    fetch_weights(w, 0);
-    if constexpr (SPS == 2) fetch_weights(w1, 1);
+    fetch_rows(0, 0, NL);
+#pragma unroll
+    for (int s = 0; s < AHEAD; ++s) fetch_weights(w[s], s);
     fetch_weight_scales(ws, 0);
     keep_scales(0);
     for (int q = 0; q < a.quads; ++q) {
         unsigned wsnext[MT], xs[NT];
 #pragma unroll
         for (int st = 0; st < SPQ; ++st) {
-            const int stage = q * SPQ + st, buffer = st & 1;
+            const int stage = q * SPQ + st, buffer = stage & 1;
             landed();
             if constexpr (MODE != kWide8) read_chunk(0, buffer);
             if (st == 0) {
@@ -380,30 +387,32 @@ __global__ __launch_bounds__(64 * WN * WM, MT * NT > 32 ? 1 : 2) void tile_kerne
                 fetch_weight_scales(wsnext, q + 1);
                 fetch_scales(q + 1);
             }
-            fetch_rows(stage + 1);                                        // (past the last stage: zeros, into the half that nothing reads any more)
-            u4 w2[MT];
-            fetch_weights(w2, (stage + 1) * SPS);
-            __builtin_amdgcn_sched_barrier(0);
-            if constexpr (MODE == kWide8) {
-                if (st == SPQ - 1) keep_scales(q + 1);
-                multiply_wide(w, xs, buffer, st);
-            } else {
 #pragma unroll
-                for (int c = 0; c < CHUNKS; ++c) {
-                    if (c + 1 < CHUNKS) read_chunk(c + 1, buffer);
-                    if (SPS == 2 && c == CHUNKS / 2) fetch_weights(w, (stage + 1) * SPS + 1);       // (the first step's registers are free now)
+            for (int u = 0; u < SPS; ++u) {
+                const int s = st * SPS + u;
+                fetch_weights(w[(s + AHEAD) % SETS], q * 4 + s + AHEAD);
+                if constexpr (MODE == kWide8) {
+                    if (u == 0) fetch_rows(stage + 1, 0, NL);             // (past the last stage: zeros, into the half that nothing reads any more)
                     __builtin_amdgcn_sched_barrier(0);
-                    multiply_chunk(c, c < CHUNKS / SPS ? w : w1, xs, st * SPS + c / (CHUNKS / SPS));
-                    if (st == SPQ - 1 && c == 0) keep_scales(q + 1);
+                    if (s == 3) keep_scales(q + 1);
+                    multiply_wide(w[s % SETS], xs, buffer, u, s);
                     __builtin_amdgcn_sched_barrier(0);
+                } else {
+#pragma unroll
+                    for (int c = 0; c < CPS; ++c) {
+                        if (u * CPS + c + 1 < SPS * CPS) read_chunk(u * CPS + c + 1, buffer);
+                        if (u == 0) fetch_rows(stage + 1, NL * c / CPS, NL * (c + 1) / CPS);
+                        __builtin_amdgcn_sched_barrier(0);
+                        multiply_chunk(u * CPS + c, w[s % SETS], xs, s);
+                        if (s == 3 && c == 0) keep_scales(q + 1);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
-                if constexpr (SPS == 2)
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) w1[i] = w[i];
             }
-#pragma unroll
-            for (int i = 0; i < MT; ++i) w[i] = w2[i];
         }
+        if constexpr (SETS == 3)                                          // four steps on, sets 1 and 2 hold what sets 0 and 1 held
+#pragma unroll
+            for (int i = 0; i < MT; ++i) w[0][i] = w[1][i], w[1][i] = w[2][i];
 #pragma unroll
         for (int i = 0; i < MT; ++i) ws[i] = wsnext[i];
     }
@@ -419,22 +428,40 @@ __global__ __launch_bounds__(64 * WN * WM, MT * NT > 32 ? 1 : 2) void tile_kerne
 #pragma unroll
         for (int j = 0; j < NT; ++j) row_scale[j] = ((const float*)a.xs)[row0 + min((wm * NT + j) * 16 + r, rows - 1)];
     const bool relu = a.act == SBN_ACT_RELU, whole = rows == RW && (int)(tile_n + 1) * CH <= a.c_out;
+    auto finished = [&](int i, int j) {
+        f4 v = acc[i][j];
+        if constexpr (FMT == SBN_FP8_ROW) v *= row_scale[j];
+        v += bias[i];
+        if (relu)
 #pragma unroll
-    for (int j = 0; j < NT; ++j) {
-        const int row = (wm * NT + j) * 16 + r;
-        T* const y = (T*)a.y + (row0 + row) * a.ldy + n0;
+            for (int c = 0; c < 4; ++c) v[c] = v[c] > 0.0f ? v[c] : 0.0f;
+        return v;
+    };
+    if (whole) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            f4 v = acc[i][j];
-            if constexpr (FMT == SBN_FP8_ROW) v *= row_scale[j];
-            v += bias[i];
-            if (relu)
+        for (int j = 0; j < NT; ++j) {
+            T* const y = (T*)a.y + (row0 + (wm * NT + j) * 16 + r) * a.ldy + first * 16;
+            if constexpr (sizeof(T) == 4) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) v[c] = v[c] > 0.0f ? v[c] : 0.0f;
-            if (whole)
-                put4(y + i * 16, 4, v);
-            else if (row < rows && n0 + i * 16 < a.c_out)
-                put4(y + i * 16, a.c_out - n0 - i * 16, v);
+                for (int i = 0; i < MT; ++i) put4(y + i * 16 + g * 4, 4, finished(i, j));
+            } else {
+                // The four lanes of a row hold 4 channels of each tile, 8 bytes.  Swapping rows of 16 lanes between two tiles leaves each
+                // lane with 8 neighbouring channels of one of them: 16-byte stores, 64 bytes of a row side by side.
+#pragma unroll
+                for (int i = 0; i < MT; i += 2) {
+                    u2 e = packed<T>(finished(i, j)), o = packed<T>(finished(i + 1, j));
+                    const auto lo = __builtin_amdgcn_permlane16_swap(e.x, o.x, false, false), hi = __builtin_amdgcn_permlane16_swap(e.y, o.y, false, false);
+                    ((Any16*)(y + (i + (g & 1)) * 16 + (g >> 1) * 8))->v = (u4){lo[0], hi[0], lo[1], hi[1]};
+                }
+            }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+            const int row = (wm * NT + j) * 16 + r;
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+                if (row < rows && n0 + i * 16 < a.c_out) put4((T*)a.y + (row0 + row) * a.ldy + n0 + i * 16, a.c_out - n0 - i * 16, finished(i, j));
         }
     }
 }
@@ -466,8 +493,6 @@ int run_linear(LinearArgs a, hipStream_t stream)
             launch_tiles<FMT, T, 4, 8, 4, 2>(b, stream);
         else if (form == 164)
             launch_tiles<FMT, T, 4, 16, 4, 1>(b, stream);
-        else if (form == 48)
-            launch_tiles<FMT, T, 4, 8, 2, 2>(b, stream);
         else if (form == 44)
             launch_tiles<FMT, T, 4, 4, 2, 2>(b, stream);
         else
