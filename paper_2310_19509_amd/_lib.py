@@ -182,6 +182,8 @@ def marshal():
         spec.loader.exec_module(m)
         m.bind(*[C.cast(f, C.c_void_p).value for f in (l.sbn_conv1x1_sparse, l.sbn_conv3x3_sparse, l.sbn_chain_output_shape,
                                                        l.sbn_pointwise_chain, l.sbn_pointwise_chain_static)])
+        m.bind_rows(*[C.cast(f, C.c_void_p).value for f in (l.sbn_quantize, l.sbn_dequantize, l.sbn_add_rmsnorm, l.sbn_linear_mx,
+                                                            l.sbn_log_probs, l.sbn_log_probs_backward)])
         _marshal = m
     return _marshal
 

@@ -140,6 +140,223 @@ PyObject* chain(PyObject*, PyObject* const* a, Py_ssize_t count)
     });
 }
 
+// ---- low-precision rows, norm, 4-bit weights, log probabilities ----------------------------------
+// The same for the calls over rows: a step of one token takes the GPU 3 to 6 us, and the Python code 8 us a call.  Arguments as the functions of api.py have them; whatever is
+// not an ordinary one, and whatever they would refuse, goes to them.
+
+struct RmsNorm {                           // sbn_rmsnorm_t
+    int64_t rows, cols;
+    const void* x; int x_type; int64_t ldx;
+    const void* residual; int r_type; int64_t ldr;
+    void* total; int64_t ldt;
+    const void* weight; float eps;
+    void* y; int64_t ldy;
+    int format; void* codes; void* scales;
+};
+typedef int (*QuantizeFn)(const void*, int, int64_t, int64_t, int64_t, int, void*, void*, void*);
+typedef int (*DequantizeFn)(const void*, const void*, int, int64_t, int64_t, void*, int, int64_t, void*);
+typedef int (*NormFn)(const RmsNorm*, void*);
+typedef int (*LinearFn)(const void*, const void*, const void*, int, int64_t, void*, int, int64_t, void*, size_t, void*);
+typedef int (*ScoreFn)(const void*, int, int64_t, int64_t, int64_t, const int64_t*, int, int, float*, float*, float*, int64_t*, float*, void*, size_t, void*);
+typedef int (*BackwardFn)(const void*, int, int64_t, int64_t, int64_t, const int64_t*, int, const float*, const float*, const float*, const float*, void*, int64_t, void*);
+QuantizeFn g_quantize;
+DequantizeFn g_dequantize;
+NormFn g_norm;
+LinearFn g_linear;
+ScoreFn g_score;
+BackwardFn g_backward;
+PyObject* g_c_out;
+
+constexpr int kMxfp4 = 4, kMxfp8 = 5, kFp8Row = 6;
+
+struct Matrix {
+    void* p;
+    int type;
+    int64_t rows, cols, ld;
+};
+bool matrix(PyObject* o, Matrix* m)
+{
+    const at::Tensor* t = plain(o);
+    if (!t || t->dim() != 2) return false;
+    switch (t->scalar_type()) {
+    case at::kFloat: m->type = 0; break;
+    case at::kBFloat16: m->type = 1; break;
+    case at::kHalf: m->type = 2; break;
+    default: return false;
+    }
+    m->p = t->data_ptr(), m->rows = t->size(0), m->cols = t->size(1), m->ld = t->stride(0);
+    if (m->rows < 1 || m->cols < 1 || (m->cols > 1 && t->stride(1) != 1)) return false;
+    if (m->rows == 1)
+        m->ld = m->cols;
+    return m->ld >= m->cols;
+}
+bool matrix(PyObject* o, Matrix* m, int64_t rows, int64_t cols) { return matrix(o, m) && m->rows == rows && m->cols == cols; }
+// A contiguous tensor of the given type and shape (cols < 0: one dimension); None where that may be.
+bool flat(PyObject* o, at::ScalarType type, int64_t rows, int64_t cols, bool optional, void** p)
+{
+    *p = nullptr;
+    if (o == Py_None) return optional;
+    const at::Tensor* t = plain(o);
+    if (!t || t->scalar_type() != type || !t->is_contiguous()) return false;
+    if (cols < 0 ? t->dim() != 1 || t->size(0) != rows : t->dim() != 2 || t->size(0) != rows || t->size(1) != cols) return false;
+    *p = t->data_ptr();
+    return true;
+}
+bool coded(PyObject* codes, PyObject* scales, int fmt, int64_t rows, int64_t cols, void** c, void** s)
+{
+    if (fmt != kMxfp4 && fmt != kMxfp8 && fmt != kFp8Row) return false;
+    const int64_t blocks = (cols + 31) / 32;
+    return flat(codes, at::kByte, rows, blocks * (fmt == kMxfp4 ? 16 : 32), false, c) &&
+           (fmt == kFp8Row ? flat(scales, at::kFloat, rows, -1, false, s) : flat(scales, at::kByte, rows, blocks, false, s));
+}
+bool memory(PyObject* o, void** p, size_t* bytes)
+{
+    *p = nullptr, *bytes = 0;
+    if (o == Py_None) return true;
+    const at::Tensor* t = plain(o);
+    if (!t || !t->is_contiguous()) return false;
+    *p = t->data_ptr(), *bytes = (size_t)t->numel() * t->element_size();
+    return true;
+}
+void* current_stream() { return (void*)c10::hip::getCurrentHIPStream().stream(); }
+template <class F>
+long unlocked(F&& call)
+{
+    long rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = call();
+    Py_END_ALLOW_THREADS
+    return rc;
+}
+bool attribute(PyObject* o, PyObject* name, int* v)
+{
+    PyObject* a = PyObject_GetAttr(o, name);
+    const bool ok = a && as_int(a, v);
+    Py_XDECREF(a);
+    return ok;
+}
+
+// quantize(x, fmt, codes, scales, stream)
+PyObject* quantize(PyObject*, PyObject* const* a, Py_ssize_t count)
+{
+    return answer([&]() -> long {
+        Matrix x;
+        int fmt;
+        void *c, *s;
+        if (count != 5 || a[4] != Py_None || !as_int(a[1], &fmt) || !matrix(a[0], &x) || !coded(a[2], a[3], fmt, x.rows, x.cols, &c, &s)) return kOther;
+        void* const st = current_stream();
+        return unlocked([&] { return g_quantize(x.p, x.type, x.rows, x.cols, x.ld, fmt, c, s, st); });
+    });
+}
+// dequantize(codes, scales, fmt, y, stream)
+PyObject* dequantize(PyObject*, PyObject* const* a, Py_ssize_t count)
+{
+    return answer([&]() -> long {
+        Matrix y;
+        int fmt;
+        void *c, *s;
+        if (count != 5 || a[4] != Py_None || !as_int(a[2], &fmt) || !matrix(a[3], &y) || !coded(a[0], a[1], fmt, y.rows, y.cols, &c, &s)) return kOther;
+        void* const st = current_stream();
+        return unlocked([&] { return g_dequantize(c, s, fmt, y.rows, y.cols, y.p, y.type, y.ld, st); });
+    });
+}
+// norm(x, weight, eps, residual, total, y, fmt, codes, scales, stream)
+PyObject* norm(PyObject*, PyObject* const* a, Py_ssize_t count)
+{
+    return answer([&]() -> long {
+        Matrix x, m;
+        RmsNorm n = {};
+        void* w;
+        if (count != 10 || a[9] != Py_None || !PyFloat_CheckExact(a[2]) || !as_int(a[6], &n.format) || !matrix(a[0], &x)) return kOther;
+        n.rows = x.rows, n.cols = x.cols, n.x = x.p, n.x_type = x.type, n.ldx = x.ld, n.eps = (float)PyFloat_AS_DOUBLE(a[2]);
+        if (!flat(a[1], at::kFloat, x.cols, -1, true, &w)) return kOther;
+        n.weight = w;
+        if (a[3] != Py_None) {
+            if (!matrix(a[3], &m, x.rows, x.cols)) return kOther;
+            n.residual = m.p, n.r_type = m.type, n.ldr = m.ld;
+        }
+        if (a[4] != Py_None) {
+            if (!matrix(a[4], &m, x.rows, x.cols) || !n.residual || m.type != n.r_type) return kOther;
+            n.total = m.p, n.ldt = m.ld;
+        }
+        if (a[5] != Py_None) {
+            if (!matrix(a[5], &m, x.rows, x.cols) || m.type != x.type) return kOther;
+            n.y = m.p, n.ldy = m.ld;
+        }
+        if (n.format && !coded(a[7], a[8], n.format, x.rows, x.cols, &n.codes, &n.scales)) return kOther;
+        void* const st = current_stream();
+        return unlocked([&] { return g_norm(&n, st); });
+    });
+}
+// linear(layer, codes, scales, fmt, y, workspace, stream)
+PyObject* linear(PyObject*, PyObject* const* a, Py_ssize_t count)
+{
+    return answer([&]() -> long {
+        Matrix y;
+        int fmt, c_in, c_out;
+        void *c, *s, *ws;
+        size_t bytes;
+        if (count != 7 || a[6] != Py_None || !as_int(a[3], &fmt) || !attribute(a[0], g_c_in, &c_in) || !attribute(a[0], g_c_out, &c_out)) return kOther;
+        void* const p = handle_of(a[0]);
+        if (!p || !matrix(a[4], &y) || y.cols != c_out || !coded(a[1], a[2], fmt, y.rows, c_in, &c, &s) || !memory(a[5], &ws, &bytes)) return kOther;
+        void* const st = current_stream();
+        return unlocked([&] { return g_linear(p, c, s, fmt, y.rows, y.p, y.type, y.ld, ws, bytes, st); });
+    });
+}
+// score(logits, targets, k, logp, lse, entropy, top_ids, top_logp, workspace, stream)
+PyObject* score(PyObject*, PyObject* const* a, Py_ssize_t count)
+{
+    return answer([&]() -> long {
+        Matrix x;
+        int k;
+        void *t = nullptr, *logp, *lse, *ent, *ids, *top, *ws;
+        size_t bytes;
+        if (count != 10 || a[9] != Py_None || !as_int(a[2], &k) || !matrix(a[0], &x)) return kOther;
+        int64_t n = 0;
+        if (a[1] != Py_None) {
+            const at::Tensor* tt = plain(a[1]);
+            if (!tt || tt->dim() != 2 || tt->size(1) > INT_MAX) return kOther;
+            n = tt->size(1);
+            if (!flat(a[1], at::kLong, x.rows, n, false, &t)) return kOther;
+        }
+        if (!flat(a[3], at::kFloat, x.rows, n, n == 0, &logp) || !flat(a[4], at::kFloat, x.rows, -1, false, &lse) || !flat(a[5], at::kFloat, x.rows, -1, true, &ent) ||
+            !flat(a[6], at::kLong, x.rows, k, k == 0, &ids) || !flat(a[7], at::kFloat, x.rows, k, k == 0, &top) || !memory(a[8], &ws, &bytes))
+            return kOther;
+        void* const st = current_stream();
+        return unlocked([&] {
+            return g_score(x.p, x.type, x.rows, x.cols, x.ld, (const int64_t*)t, (int)n, k, (float*)logp, (float*)lse, (float*)ent, (int64_t*)ids, (float*)top, ws, bytes, st);
+        });
+    });
+}
+// backward(logits, targets, lse, entropy, g_logp, g_entropy, grad, stream)
+PyObject* backward(PyObject*, PyObject* const* a, Py_ssize_t count)
+{
+    return answer([&]() -> long {
+        Matrix x, g;
+        void *t, *lse, *ent, *gl, *gh;
+        if (count != 8 || a[7] != Py_None || a[1] == Py_None || !matrix(a[0], &x) || !matrix(a[6], &g, x.rows, x.cols) || g.type != x.type) return kOther;
+        const at::Tensor* tt = plain(a[1]);
+        if (!tt || tt->dim() != 2 || tt->size(1) > INT_MAX) return kOther;
+        const int64_t n = tt->size(1);
+        if (!flat(a[1], at::kLong, x.rows, n, false, &t) || !flat(a[2], at::kFloat, x.rows, -1, false, &lse) || !flat(a[3], at::kFloat, x.rows, -1, a[5] == Py_None, &ent) ||
+            !flat(a[4], at::kFloat, x.rows, n, n == 0, &gl) || !flat(a[5], at::kFloat, x.rows, -1, true, &gh))
+            return kOther;
+        void* const st = current_stream();
+        return unlocked([&] {
+            return g_backward(x.p, x.type, x.rows, x.cols, x.ld, (const int64_t*)t, (int)n, (const float*)lse, (const float*)ent, (const float*)gl, (const float*)gh, g.p, g.ld, st);
+        });
+    });
+}
+
+// bind_rows(addresses of sbn_quantize, sbn_dequantize, sbn_add_rmsnorm, sbn_linear_mx, sbn_log_probs, sbn_log_probs_backward)
+PyObject* bind_rows(PyObject*, PyObject* args)
+{
+    Py_ssize_t f[6];
+    if (!PyArg_ParseTuple(args, "nnnnnn", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5])) return nullptr;
+    g_quantize = (QuantizeFn)f[0], g_dequantize = (DequantizeFn)f[1], g_norm = (NormFn)f[2], g_linear = (LinearFn)f[3], g_score = (ScoreFn)f[4], g_backward = (BackwardFn)f[5];
+    Py_RETURN_NONE;
+}
+
 // bind(addresses of sbn_conv1x1_sparse, sbn_conv3x3_sparse, sbn_chain_output_shape, sbn_pointwise_chain, sbn_pointwise_chain_static)
 PyObject* bind(PyObject*, PyObject* args)
 {
@@ -152,6 +369,13 @@ PyObject* bind(PyObject*, PyObject* args)
 PyMethodDef methods[] = {{"layer", (PyCFunction)(void*)layer, METH_FASTCALL, nullptr},
                          {"chain", (PyCFunction)(void*)chain, METH_FASTCALL, nullptr},
                          {"bind", bind, METH_VARARGS, nullptr},
+                         {"bind_rows", bind_rows, METH_VARARGS, nullptr},
+                         {"quantize", (PyCFunction)(void*)quantize, METH_FASTCALL, nullptr},
+                         {"dequantize", (PyCFunction)(void*)dequantize, METH_FASTCALL, nullptr},
+                         {"norm", (PyCFunction)(void*)norm, METH_FASTCALL, nullptr},
+                         {"linear", (PyCFunction)(void*)linear, METH_FASTCALL, nullptr},
+                         {"score", (PyCFunction)(void*)score, METH_FASTCALL, nullptr},
+                         {"backward", (PyCFunction)(void*)backward, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -162,5 +386,6 @@ PyMODINIT_FUNC PyInit__marshal()
     g_handle = PyUnicode_InternFromString("handle");
     g_dims = PyUnicode_InternFromString("_dims");
     g_c_in = PyUnicode_InternFromString("c_in");
-    return g_handle && g_dims && g_c_in ? PyModule_Create(&module) : nullptr;
+    g_c_out = PyUnicode_InternFromString("c_out");
+    return g_handle && g_dims && g_c_in && g_c_out ? PyModule_Create(&module) : nullptr;
 }

@@ -661,6 +661,18 @@ def _bytes_of(workspace, what: str = "workspace"):
     return workspace.data_ptr(), workspace.numel() * workspace.element_size()
 
 
+_rows_native = None
+
+
+def _rows_calls():
+    """The entry points of _marshal.cpp for the calls over rows, or None where it cannot be used."""
+    global _rows_native
+    if _rows_native is None:
+        _native_calls()                           # (loads it, or warns once)
+        _rows_native = (_lib._marshal,)
+    return _rows_native
+
+
 def sbn_quantized_bytes(fmt: int, rows: int, cols: int):
     """(bytes of codes, bytes of scales) for rows x cols."""
     a, b = C.c_size_t(), C.c_size_t()
@@ -677,18 +689,33 @@ def sbn_quantized_empty(fmt: int, rows: int, cols: int, device="cuda"):
 
 
 def sbn_quantize(x, fmt: int, codes, scales, stream=None) -> None:
+    m = (_rows_native or _rows_calls())[0]
+    if m is not None:
+        rc = m.quantize(x, fmt, codes, scales, stream)
+        if rc is not None:
+            return _check(rc) if rc else None
     xp, xt, rows, cols, ld = _matrix(x, "x")
     cp, sp = _codes(codes, scales, fmt, rows, cols)
     _check(_lib.lib().sbn_quantize(xp, xt, rows, cols, ld, fmt, cp, sp, _stream(stream)))
 
 
 def sbn_dequantize(codes, scales, fmt: int, y, stream=None) -> None:
+    m = (_rows_native or _rows_calls())[0]
+    if m is not None:
+        rc = m.dequantize(codes, scales, fmt, y, stream)
+        if rc is not None:
+            return _check(rc) if rc else None
     yp, yt, rows, cols, ld = _matrix(y, "y")
     cp, sp = _codes(codes, scales, fmt, rows, cols)
     _check(_lib.lib().sbn_dequantize(cp, sp, fmt, rows, cols, yp, yt, ld, _stream(stream)))
 
 
 def sbn_add_rmsnorm(x, weight, eps: float, residual=None, total=None, y=None, fmt: int = 0, codes=None, scales=None, stream=None) -> None:
+    m = (_rows_native or _rows_calls())[0]
+    if m is not None:
+        rc = m.norm(x, weight, eps, residual, total, y, fmt, codes, scales, stream)
+        if rc is not None:
+            return _check(rc) if rc else None
     import torch
     a = _lib.RmsNorm()
     a.x, a.x_type, a.rows, a.cols, a.ldx = _matrix(x, "x")
@@ -775,6 +802,11 @@ def sbn_linear_mx_workspace(p: MxPacked, fmt: int, rows: int) -> int:
 
 
 def sbn_linear_mx(p: MxPacked, codes, scales, fmt: int, y, workspace=None, stream=None) -> None:
+    m = (_rows_native or _rows_calls())[0]
+    if m is not None:
+        rc = m.linear(p, codes, scales, fmt, y, workspace, stream)
+        if rc is not None:
+            return _check(rc) if rc else None
     yp, yt, rows, _, ld = _matrix(y, "y", y.shape[0], p.c_out)
     cp, sp = _codes(codes, scales, fmt, rows, p.c_in)
     wp, wb = _bytes_of(workspace)
@@ -789,6 +821,11 @@ def sbn_log_probs_workspace(rows: int, cols: int, k: int) -> int:
 
 def sbn_log_probs(logits, targets, k: int, logp, lse, entropy=None, top_ids=None, top_logp=None, workspace=None, stream=None) -> None:
     """targets int64 [rows][n] (or None); logp [rows][n], lse and entropy [rows], top_ids (int64) and top_logp [rows][k]."""
+    m = (_rows_native or _rows_calls())[0]
+    if m is not None:
+        rc = m.score(logits, targets, k, logp, lse, entropy, top_ids, top_logp, workspace, stream)
+        if rc is not None:
+            return _check(rc) if rc else None
     import torch
     xp, xt, rows, cols, ld = _matrix(logits, "logits")
     n = 0 if targets is None else targets.shape[-1]
@@ -803,6 +840,11 @@ def sbn_log_probs(logits, targets, k: int, logp, lse, entropy=None, top_ids=None
 
 def sbn_log_probs_backward(logits, targets, lse, entropy, g_logp, g_entropy, grad, stream=None) -> None:
     """grad (the logits' type; may be the logits themselves) from the gradients of logp and, if not None, of the entropy."""
+    m = (_rows_native or _rows_calls())[0]
+    if m is not None:
+        rc = m.backward(logits, targets, lse, entropy, g_logp, g_entropy, grad, stream)
+        if rc is not None:
+            return _check(rc) if rc else None
     import torch
     xp, xt, rows, cols, ld = _matrix(logits, "logits")
     gp, gt, _, _, ldg = _matrix(grad, "grad", rows, cols)

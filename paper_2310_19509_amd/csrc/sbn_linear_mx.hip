@@ -137,74 +137,113 @@ __device__ inline void finish4(const LinearArgs& a, long long row, int n, f4 v)
     put4((T*)a.y + row * a.ldy + n, a.c_out - n, v);
 }
 
-// 16 rows x 16 NT output channels to a workgroup, whose four waves take every fourth quad of steps (512 input channels) and join
-// their sums in LDS.
-template <int FMT, class T, int NT>
-__global__ __launch_bounds__(256) void rows_kernel(const LinearArgs a)
+enum { kNarrow, kScaled8, kWide8 };         // 4-bit rows; 8-bit rows on scaled multiplies; 8-bit rows as bfloat16
+
+// Few rows: 16 RT rows x 16 NT output channels to a workgroup, whose WAVES waves take the quads of steps (512 input channels) in turn and
+// join their sums in LDS.  Bound by reading the weights once, which go from memory to registers in one 16-byte load per lane and
+// step; the rows, read again by every workgroup, come from L2.
+template <int MODE, bool BLOCKS, class T, int NT, int RT, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(const LinearArgs a)
 {
-    __shared__ f4 sums[3][NT][64];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, g = lane >> 4;
+    __shared__ f4 sums[WAVES][NT * RT][64];
+    const int wave = (int)threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int tile0 = blockIdx.x * NT;
-    const long long row = (long long)blockIdx.y * 16 + (lane & 15);
-    const bool live = row < a.rows;
-    const uint8_t* const x = a.x + (live ? row : 0) * a.blocks * (FMT == SBN_MXFP4 ? 16 : 32);
-    const uint8_t* const xs = a.xs + (live ? row : 0) * a.blocks;
-    f4 acc[NT] = {};
-    for (int q = wave; q < a.quads; q += 4) {
-        unsigned ws[NT];
+    const long long row0 = (long long)blockIdx.y * (16 * RT);
+    constexpr int BB = MODE == kNarrow ? 16 : 32;                         // bytes of a block of a row
+    const uint8_t *x[RT], *xs[RT];
+    bool live[RT];
+#pragma unroll
+    for (int j = 0; j < RT; ++j) {
+        const long long row = row0 + j * 16 + r;
+        live[j] = row < a.rows;
+        x[j] = a.x + (live[j] ? row : row0) * a.blocks * BB;
+        xs[j] = a.xs + (live[j] ? row : row0) * a.blocks;
+    }
+    f4 acc[NT][RT] = {};
+    for (int q = wave; q < a.quads; q += WAVES) {
+        unsigned ws[NT], sx[RT];
+        u4 w[NT][4];
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
-            const int tile = min(tile0 + t, a.tile_rows - 1);
-            ws[t] = ((const unsigned*)a.ws)[((long long)tile * a.quads + q) * 64 + lane];
+            const long long tile = min(tile0 + t, a.tile_rows - 1);
+            ws[t] = ((const unsigned*)a.ws)[(tile * a.quads + q) * 64 + lane];
+#pragma unroll
+            for (int s = 0; s < 4; ++s) w[t][s] = ((const u4*)a.w)[(tile * a.steps + min(q * 4 + s, a.steps - 1)) * 64 + lane];     // (past c_in: the scale is 0)
+        }
+#pragma unroll
+        for (int j = 0; j < RT; ++j) {
+            sx[j] = 127u * 0x01010101u;
+            if constexpr (BLOCKS) {
+                if (q * 16 + 16 <= a.blocks) {
+                    const u4 d = ((const Bytes16*)(xs[j] + q * 16))->v;
+                    const unsigned sel = (unsigned)g | (unsigned)(g + 4) << 8;
+                    const unsigned lo = __builtin_amdgcn_perm(d[1], d[0], sel), hi = __builtin_amdgcn_perm(d[3], d[2], sel);
+                    sx[j] = __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+                } else {
+                    sx[j] = 0;
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) {
+                        const int block = q * 16 + s * 4 + g;
+                        const unsigned v = xs[j][min(block, a.blocks - 1)];
+                        sx[j] |= (block < a.blocks ? v : 0u) << 8 * s;
+                    }
+                }
+            }
         }
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
-            const int step = q * 4 + s;
-            if (step >= a.steps) break;
-            u4 w[NT];
+            if constexpr (MODE == kWide8) {
+                b8 B[RT][4];
+                const int block = (q * 4 + s) * 4 + g;
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const int tile = min(tile0 + t, a.tile_rows - 1);
-                w[t] = ((const u4*)a.w)[((long long)tile * a.steps + step) * 64 + lane];
-            }
-            const int block = step * 4 + g;
-            const bool in = live && block < a.blocks;
-            if constexpr (FMT == SBN_MXFP4) {
-                const u4 c = in ? ((const u4*)x)[block] : (u4){};
-                const int sx = in ? xs[block] : 0;
-                const i8v B = {(int)c.x, (int)c.y, (int)c.z, (int)c.w, 0, 0, 0, 0};
+                for (int j = 0; j < RT; ++j) {
+                    u4 c[2] = {};
+                    if (live[j] && block < a.blocks) c[0] = ((const u4*)x[j])[block * 2], c[1] = ((const u4*)x[j])[block * 2 + 1];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const i8v A = {(int)w[t].x, (int)w[t].y, (int)w[t].z, (int)w[t].w, 0, 0, 0, 0};
-                    acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(A, B, acc[t], 4, 4, 0, (int)(ws[t] >> 8 * s & 255u), 0, sx);
+                    for (int i = 0; i < 4; ++i) B[j][i] = wide8(c[i >> 1][(i & 1) * 2], c[i >> 1][(i & 1) * 2 + 1], mx_scale(sx[j] >> 8 * s & 255u));
                 }
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const b8 A = wide4(w[t][s][i], mx_scale(ws[t] >> 8 * s & 255u));
+#pragma unroll
+                        for (int j = 0; j < RT; ++j) acc[t][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(A, B[j][i], acc[t][j], 0, 0, 0);
+                    }
             } else {
-                u4 c[2] = {};
-                float sx = 1.0f;
-                if (in) {
-                    c[0] = ((const u4*)x)[block * 2], c[1] = ((const u4*)x)[block * 2 + 1];
-                    if constexpr (FMT == SBN_MXFP8) sx = mx_scale(xs[block]);
-                }
-                b8 B[4];
+                i8v B[RT];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) B[i] = wide8(c[i >> 1][(i & 1) * 2], c[i >> 1][(i & 1) * 2 + 1], sx);
+                for (int j = 0; j < RT; ++j) {
+                    // pieces of 16 bytes: the block's own (4 bits), or g and 4 + g of the step's eight
+                    const int p = MODE == kNarrow ? (q * 4 + s) * 4 + g : (q * 4 + s) * 8 + g, end = MODE == kNarrow ? a.blocks : a.blocks * 2;
+                    u4 lo = {}, hi = {};
+                    if (live[j] && p < end) lo = ((const u4*)x[j])[p];
+                    if constexpr (MODE == kScaled8)
+                        if (live[j] && p + 4 < end) hi = ((const u4*)x[j])[p + 4];
+                    B[j] = (i8v){(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
+                }
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    const float sw = mx_scale(ws[t] >> 8 * s & 255u);
+                    const i8v A = {(int)w[t][s].x, (int)w[t][s].y, (int)w[t][s].z, (int)w[t][s].w, 0, 0, 0, 0};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wide4(w[t][i], sw), B[i], acc[t], 0, 0, 0);
+                    for (int j = 0; j < RT; ++j) acc[t][j] = scaled_mma<MODE == kNarrow ? 4 : 0>(A, B[j], acc[t][j], s, ws[t], sx[j]);
                 }
             }
         }
     }
-    if (wave)
 #pragma unroll
-        for (int t = 0; t < NT; ++t) sums[wave - 1][t][lane] = acc[t];
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int j = 0; j < RT; ++j) sums[wave][t * RT + j][lane] = acc[t][j];
     __syncthreads();
-    if (wave == 0)
+    constexpr int FMT = MODE == kNarrow ? SBN_MXFP4 : BLOCKS ? SBN_MXFP8 : SBN_FP8_ROW;
+    for (int p = wave; p < NT * RT; p += WAVES) {
+        const int t = p / RT, j = p % RT;
+        f4 v = sums[0][p][lane];
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-            if (tile0 + t < a.tile_rows) finish4<FMT, T>(a, row, (tile0 + t) * 16 + g * 4, acc[t] + sums[0][t][lane] + sums[1][t][lane] + sums[2][t][lane]);
+        for (int k = 1; k < WAVES; ++k) v += sums[k][p][lane];
+        if (tile0 + t < a.tile_rows) finish4<FMT, T>(a, row0 + j * 16 + r, (tile0 + t) * 16 + g * 4, v);
+    }
 }
 
 // One 16-byte piece per lane from a buffer straight to LDS, lane l's at `lds` + 16 l.  In inline assembly because the compiler, which cannot tell
@@ -225,7 +264,6 @@ __device__ inline unsigned uniform(unsigned v) { return (unsigned)__builtin_amdg
 // Sixteen-byte pieces of a row lie at piece ^ (row & 7), which spreads the reads of eight rows over all banks.
 // Scales of rows are turned, four steps at a time, into words that hold a lane's bytes of four steps, as the weights' are.
 // The last four steps are whole: past c_in they multiply zeros (leaving the loop among them would cost registers for every sum).
-enum { kNarrow, kScaled8, kWide8 };         // 4-bit rows; 8-bit rows on scaled multiplies; 8-bit rows as bfloat16
 template <int MODE, bool BLOCKS, class T, int MT, int NT, int WN, int WM>
 __global__ __launch_bounds__(64 * WN * WM, MT * NT > 32 ? 1 : 2) void tile_kernel(const LinearArgs a, const unsigned tiles_n, const unsigned tiles_m)
 {
@@ -475,37 +513,74 @@ void launch_tiles(const LinearArgs& a, hipStream_t stream)
     tile_kernel<MODE, FMT != SBN_FP8_ROW, T, MT, NT, WN, WM><<<(tn * tm + 7) / 8 * 8, 64 * WN * WM, 0, stream>>>(a, tn, tm);
 }
 
-template <int FMT, class T>
-int run_linear(LinearArgs a, hipStream_t stream)
+template <int FMT, class T, int NT, int RT>
+void launch_few(const LinearArgs& a, hipStream_t stream)
 {
-    const long long all = a.rows, most = 65535ll * 16;
+    constexpr int MODE = FMT == SBN_MXFP4 ? kNarrow : sizeof(T) == 4 ? kWide8 : kScaled8;
+    const dim3 grid((unsigned)((a.tile_rows + NT - 1) / NT), (unsigned)((a.rows + 16 * RT - 1) / (16 * RT)));
+    few_rows_kernel<MODE, FMT != SBN_FP8_ROW, T, NT, RT, 4><<<grid, 256, 0, stream>>>(a);
+}
+
+// Which kernel, by what each takes, in microseconds, measured with both over 32 to 8192 rows and 1000 to 32768 channels.
+//   few rows (16 or 32 of them to a workgroup): the weights once more for every 32 rows: 3 + operations / rate, the rate 750, 470
+//     or 500 TFLOP/s (4-bit rows, 8-bit rows, 8-bit rows to 32 bits).  Of 16 rows at most nothing else comes near:
+//     8192 -> 32768 channels, 16 rows in 8 bits: 29 us, 42 in tiles.
+//   tiles of 128 x 128: 2 + 0.36, 0.5 or 1 per 128 input channels for as many tiles as there are compute units.
+//   tiles of 256 x 256: 8/3 of a round of those, for four times the work: 8192^3 in 4 bits 255 us, 345 in the small ones; 2048 x 4096 x 4096, half
+//     a round, 32 us and 25.  Not for 32-bit results of 8-bit rows, where the conversions to bfloat16 leave no registers.
+int form_for(const LinearArgs& a, int mode, int cus)
+{
+    const int forced = forced_kernel_form(SBN_LINEAR_MX);
+    const auto groups = [&](int side) { return ((long long)a.c_out + side - 1) / side * ((a.rows + side - 1) / side); };
+    const auto rounds = [&](int side) { return (groups(side) + cus - 1) / cus; };
+    // a tile of rows has to lie within 31 bits, the scales to fill a load
+    const bool tiles = (long long)a.blocks * 32 * 256 < 1ll << 31 && a.rows * a.blocks >= 16;
+    const int wide = mode == kNarrow ? 164 : mode == kScaled8 ? 88 : 44, few = a.rows > 16 ? 22 : a.tile_rows >= 2 * cus ? 21 : 11;
+    if (forced == 11 || forced == 21 || forced == 22) return forced;
+    if (forced) return !tiles ? few : forced == 44 ? 44 : wide;
+    if (!tiles || a.rows <= 16) return few;
+    const double rate[] = {750e6, 470e6, 500e6}, step[] = {0.36, 0.5, 1.0};
+    const double by_few = 3.0 + 2.0 * (double)((a.rows + 31) / 32 * 32) * a.c_out * a.steps * 128.0 / rate[mode];
+    const double by_tiles = (double)rounds(128) * (2.0 + step[mode] * a.steps);
+    if (by_few <= by_tiles) return few;
+    return 8 * rounds(256) <= 3 * rounds(128) ? wide : 44;
+}
+
+template <int FMT, class T>
+int run_linear(LinearArgs a, int cus, hipStream_t stream)
+{
+    constexpr int MODE = FMT == SBN_MXFP4 ? kNarrow : sizeof(T) == 4 ? kWide8 : kScaled8;
+    const long long all = a.rows;
+    // rows a launch: a workgroup index below 2^23, for 128 x 128 tiles, and 65535 rows of workgroups of 16
+    const long long most = std::min(65535ll * 16, std::max(1ll, (1ll << 23) / ((a.c_out + 127) / 128)) * 128);
     for (long long r0 = 0; r0 < all; r0 += most) {
         LinearArgs b = a;
         b.rows = std::min(most, all - r0);
         b.x = a.x + r0 * a.blocks * (FMT == SBN_MXFP4 ? 16 : 32);
         b.xs = a.xs + r0 * (FMT == SBN_FP8_ROW ? 4 : a.blocks);
         b.y = (T*)a.y + r0 * a.ldy;
-        int form = forced_kernel_form(SBN_LINEAR_MX);
-        if (!form) form = b.rows > 64 ? 88 : 1;
-        if ((long long)a.blocks * 32 * 256 >= 1ll << 31 || b.rows * a.blocks < 16) form = 1;      // (a tile of rows has to lie within 31 bits, the scales to fill a load)
-        const dim3 grid((unsigned)a.tile_rows, (unsigned)((b.rows + 15) / 16));
-        if (form == 88)
-            launch_tiles<FMT, T, 4, 8, 4, 2>(b, stream);
-        else if (form == 164)
-            launch_tiles<FMT, T, 4, 16, 4, 1>(b, stream);
-        else if (form == 44)
-            launch_tiles<FMT, T, 4, 4, 2, 2>(b, stream);
-        else
-            rows_kernel<FMT, T, 1><<<grid, 256, 0, stream>>>(b);
+        const int form = form_for(b, MODE, cus);
+        switch (form) {
+        case 164:
+            if constexpr (MODE == kNarrow) launch_tiles<FMT, T, 4, 16, 4, 1>(b, stream);
+            break;
+        case 88:
+            if constexpr (MODE == kScaled8) launch_tiles<FMT, T, 4, 8, 4, 2>(b, stream);
+            break;
+        case 44: launch_tiles<FMT, T, 4, 4, 2, 2>(b, stream); break;
+        case 22: launch_few<FMT, T, 2, 2>(b, stream); break;
+        case 21: launch_few<FMT, T, 2, 1>(b, stream); break;
+        default: launch_few<FMT, T, 1, 1>(b, stream); break;
+        }
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return fail(SBN_EHIP, "sbn_linear_mx: %s", hipGetErrorString(e));
     }
     return SBN_OK;
 }
 template <int FMT>
-int run_linear(const LinearArgs& a, int y_type, hipStream_t stream)
+int run_linear(const LinearArgs& a, int y_type, int cus, hipStream_t stream)
 {
-    return y_type == SBN_F32 ? run_linear<FMT, float>(a, stream) : y_type == SBN_BF16 ? run_linear<FMT, __bf16>(a, stream)
-                                                                                     : run_linear<FMT, _Float16>(a, stream);
+    return y_type == SBN_F32 ? run_linear<FMT, float>(a, cus, stream) : y_type == SBN_BF16 ? run_linear<FMT, __bf16>(a, cus, stream)
+                                                                                          : run_linear<FMT, _Float16>(a, cus, stream);
 }
 
 }  // namespace
@@ -530,8 +605,8 @@ int launch_linear_mx(const sbn_mx* p, const void* codes, const void* scales, int
     a.y = y, a.rows = rows, a.ldy = ldy, a.c_out = p->c_out, a.blocks = p->blocks, a.steps = p->steps, a.quads = p->quads;
     a.tile_rows = p->tile_rows, a.act = p->act;
     const hipStream_t s = (hipStream_t)stream;
-    return format == SBN_MXFP4 ? run_linear<SBN_MXFP4>(a, y_type, s) : format == SBN_MXFP8 ? run_linear<SBN_MXFP8>(a, y_type, s)
-                                                                                         : run_linear<SBN_FP8_ROW>(a, y_type, s);
+    return format == SBN_MXFP4 ? run_linear<SBN_MXFP4>(a, y_type, p->cus, s) : format == SBN_MXFP8 ? run_linear<SBN_MXFP8>(a, y_type, p->cus, s)
+                                                                                                 : run_linear<SBN_FP8_ROW>(a, y_type, p->cus, s);
 }
 
 }  // namespace sbn
