@@ -53,8 +53,8 @@ __device__ inline Stat wave_join(Stat a)
     }
     return a;
 }
-// Adds eight columns.  NaN and +infinity make s NaN: e^(inf - inf).
-__device__ inline void add(Stat& a, const float (&v)[8])
+// Adds eight columns, returns the largest of them that is no NaN.  NaN and +infinity make s NaN: e^(inf - inf).
+__device__ inline float add(Stat& a, const float (&v)[8])
 {
     float top = v[0];
 #pragma unroll
@@ -66,6 +66,7 @@ __device__ inline void add(Stat& a, const float (&v)[8])
         a.s += e;
         a.t = __builtin_fmaf(e, bounded(d), a.t);
     }
+    return top;
 }
 
 // The order of the alternatives: larger logits first, of equal ones the lower column.  NaN is above +infinity, -0 equals 0.
@@ -100,36 +101,69 @@ __device__ inline void wave_fence()
     __builtin_amdgcn_wave_barrier();
 }
 
+__device__ inline Key lane_key(Key v, int lane)
+{
+    return (Key)(unsigned)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (unsigned)__builtin_amdgcn_readlane((int)(unsigned)v, lane);
+}
+// Where a lane's key stands among the n lanes' (all differ): the number of larger ones.
+__device__ inline int place_of(Key v, int n)
+{
+    int place = 0;
+    for (int i = 0; i < n; ++i) place += lane_key(v, i) > v;
+    return place;
+}
+// The k largest of up to 64 R keys, to the front of the list in any order: the k-th largest is found bit by bit, from the first in which the keys differ.
+template <int R>
+__device__ inline void keep_by_bits(Key* list, int n, int k)
+{
+    const int lane = threadIdx.x & 63;
+    Key v[R], differ = 0;
+#pragma unroll
+    for (int i = 0; i < R; ++i) v[i] = i * 64 + lane < n ? list[i * 64 + lane] : 0;                  // (no key is 0)
+    const Key first = lane_key(v[0], 0);
+#pragma unroll
+    for (int i = 0; i < R; ++i) differ |= v[i] ? v[i] ^ first : 0;
+#pragma unroll
+    for (int d = 32; d; d >>= 1)
+        differ |= (Key)(unsigned)__shfl_xor((int)(differ >> 32), d) << 32 | (unsigned)__shfl_xor((int)(unsigned)differ, d);
+    const int top = 63 - __clzll((long long)differ);                                                 // (n > k >= 1: some differ)
+    Key r = top == 63 ? 0 : first >> (top + 1) << (top + 1);
+    for (int b = top; b >= 0; --b) {
+        const Key trial = r | (Key)1 << b;
+        int count = 0;
+#pragma unroll
+        for (int i = 0; i < R; ++i) count += __popcll(__ballot(v[i] >= trial));
+        if (count >= k) r = trial;
+        if (count == k) break;
+    }
+    int at = 0;
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+        const unsigned long long keep = __ballot(v[i] >= r);
+        if (v[i] >= r) list[at + __popcll(keep & ((1ull << lane) - 1))] = v[i];
+        at += __popcll(keep);
+    }
+}
 // Moves the k largest of a wave's n keys (n <= kHold) to the front of its list, in any order; fewer than k are left as they are.
 // Returns their number.  All keys differ.
 __device__ inline int keep_largest(Key* list, int n, int k)
 {
     wave_fence();
     if (n <= k) return n;
-    const int lane = threadIdx.x & 63, rounds = (n + 63) / 64;
-    Key v[kHold / 64];
-#pragma unroll
-    for (int i = 0; i < kHold / 64; ++i) v[i] = i < rounds && i * 64 + lane < n ? list[i * 64 + lane] : 0;      // (no key is 0)
-    Key r = 0;
-    for (int b = 63; b >= 0; --b) {
-        const Key trial = r | (Key)1 << b;
-        int count = 0;
-#pragma unroll
-        for (int i = 0; i < kHold / 64; ++i)
-            if (i < rounds) count += __popcll(__ballot(v[i] >= trial));
-        if (count >= k) r = trial;
-        if (count == k) break;
+    if (n <= 64) {
+        const int lane = threadIdx.x & 63;
+        const Key v = lane < n ? list[lane] : 0;
+        const int place = place_of(v, n);
+        if (place < k) list[place] = v;                                   // (lanes past n have n larger ones)
+    } else if (n <= 128) {
+        keep_by_bits<2>(list, n, k);
+    } else if (n <= 256) {
+        keep_by_bits<4>(list, n, k);
+    } else {
+        keep_by_bits<kHold / 64>(list, n, k);
     }
-    int at = 0;
-#pragma unroll
-    for (int i = 0; i < kHold / 64; ++i)
-        if (i < rounds) {
-            const unsigned long long keep = __ballot(v[i] >= r);
-            if (v[i] >= r) list[at + __popcll(keep & ((1ull << lane) - 1))] = v[i];
-            at += __popcll(keep);
-        }
     wave_fence();
-    return at;
+    return k;
 }
 
 // A wave's search for the k largest keys of the columns that it is shown in ascending order.
@@ -144,13 +178,10 @@ struct Search {
         const float b = logit_of(kth_of_lanes(order_of(lane_top), k));
         if (!(least >= b)) least = b;
     }
+    // top: the largest of v that is no NaN; odd: whether a NaN may be among them.
     // `equal`: columns equal to the bound count (those that it was taken from); later ones lose to them.
-    __device__ void show(const float (&v)[8], unsigned col, bool equal)
+    __device__ void show(const float (&v)[8], float top, bool odd, unsigned col, bool equal)
     {
-        float top = v[0];
-        bool odd = v[0] != v[0];
-#pragma unroll
-        for (int j = 1; j < 8; ++j) top = fmaxf(top, v[j]), odd |= v[j] != v[j];
         if (!__any(odd || (equal ? !(top < least) : !(top <= least)))) return;
         if (n > kHold - kStep) {
             n = keep_largest(list, n, k);
@@ -218,10 +249,9 @@ __device__ inline void finish_row(const Args& a, const T* x, long long row, cons
             r = log_prob(Elem<T>::get(x[c]));
         a.logp[row * a.n_targets + j] = r;
     }
-    if (a.k && threadIdx.x < 64) {                                        // n = k keys: every one's place is the number of larger ones
+    if (a.k && threadIdx.x < 64) {
         const Key mine = lane < n ? list[lane] : 0;
-        int place = 0;
-        for (int i = 0; i < n; ++i) place += list[i] > mine;
+        const int place = place_of(mine, n);
         if (lane < n) {
             a.top_ids[row * a.k + place] = (int64_t)(unsigned)~(unsigned)mine;
             a.top_logp[row * a.k + place] = log_prob(logit_of((unsigned)(mine >> 32)));
@@ -269,18 +299,18 @@ __global__ __launch_bounds__(64 * kWaves) void score_kernel(const T* __restrict_
         Raw<T> raw[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) raw[u] = fetch_unit(x, (c0 + u * kTurn) / 8 + lane, end);
-        float v[U][8];
+        float v[U][8], top[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             expand_unit(raw[u], x, (c0 + u * kTurn) / 8 + lane, end, v[u], -__builtin_inff());
-            add(st, v[u]);
+            top[u] = add(st, v[u]);
         }
         if constexpr (TOP) {
             const bool bound = turn == next_bound;                        // at turns 0, 1, 3, 7, ...: the bound rises with the logarithm of what was seen
             if (bound) next_bound = 2 * turn + 1;
             if (bound) find.bound(st.s != st.s ? __builtin_nanf("") : st.m == kLow ? -__builtin_inff() : st.m);
 #pragma unroll
-            for (int u = 0; u < U; ++u) find.show(v[u], c0 + u * kTurn + lane * 8, bound);
+            for (int u = 0; u < U; ++u) find.show(v[u], top[u], st.s != st.s, c0 + u * kTurn + lane * 8, bound);
         }
     }
     st = wave_join(st);
