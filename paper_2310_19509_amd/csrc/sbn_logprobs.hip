@@ -83,13 +83,18 @@ __device__ inline float logit_of(unsigned order)
 typedef unsigned long long Key;                 // order << 32 | ~column: of two equal logits the lower column is the larger key
 __device__ inline Key key_of(float x, unsigned col) { return (Key)order_of(x) << 32 | (unsigned)~col; }
 
-// The k-th largest of the 64 lanes' values (k in 1 .. 64), the same on all lanes: bit by bit, the largest value that at least k lanes reach.
-__device__ inline unsigned kth_of_lanes(unsigned v, int k)
+// A value that the k-th largest of the lanes' N values (k in 1 .. 64) reaches, the same on all lanes: its upper 16 bits, bit by bit (all there is of bfloat16;
+// of longer logits a little less than the k-th largest, so that a few more columns pass).
+template <int N>
+__device__ inline unsigned kth_of_lanes(const unsigned (&v)[N], int k)
 {
     unsigned r = 0;
-    for (int b = 31; b >= 0; --b) {
+    for (int b = 31; b >= 16; --b) {
         const unsigned trial = r | 1u << b;
-        if (__popcll(__ballot(v >= trial)) >= k) r = trial;
+        int count = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) count += __popcll(__ballot(v[i] >= trial));
+        if (count >= k) r = trial;
     }
     return r;
 }
@@ -170,43 +175,38 @@ __device__ inline int keep_largest(Key* list, int n, int k)
 struct Search {
     Key* list;
     int n, k;
-    float least;                                // what at least k columns seen reach; NaN: not known yet
-    __device__ void start(Key* l, int k_) { list = l, n = 0, k = k_, least = __builtin_nanf(""); }
-    // A bound from the lanes' largest values so far (NaN counts as above all, and then as no bound).
-    __device__ void bound(float lane_top)
+    unsigned limit;                             // columns of the row: what lies past them is no column
+    float bound;                                // what at least k columns of the row reach; NaN: not known.  Smaller ones are out.
+    float least;                                // what at least k columns on the list, all before the ones to come, reach: equal ones are out too
+    __device__ void start(Key* l, int k_, unsigned limit_) { list = l, n = 0, k = k_, limit = limit_, bound = least = __builtin_nanf(""); }
+    __device__ void raise_bound(unsigned order)
     {
-        const float b = logit_of(kth_of_lanes(order_of(lane_top), k));
-        if (!(least >= b)) least = b;
+        const float b = logit_of(order);        // (the upper bits of NaN and of -infinity are NaN's, and then no bound)
+        if (!(bound >= b)) bound = b;
     }
     // top: the largest of v that is no NaN; odd: whether a NaN may be among them.
-    // `equal`: columns equal to the bound count (those that it was taken from); later ones lose to them.
-    __device__ void show(const float (&v)[8], float top, bool odd, unsigned col, bool equal)
+    __device__ void show(const float (&v)[8], float top, bool odd, unsigned col)
     {
-        if (!__any(odd || (equal ? !(top < least) : !(top <= least)))) return;
+        if (!__any(odd || (!(top < bound) && !(top <= least)))) return;
         if (n > kHold - kStep) {
             n = keep_largest(list, n, k);
-            bound_from_list();
+            const int lane = threadIdx.x & 63;
+            unsigned low = lane < n ? (unsigned)(list[lane] >> 32) : 0xFFFFFFFFu;
+#pragma unroll
+            for (int d = 32; d; d >>= 1) low = min(low, (unsigned)__shfl_xor((int)low, d));
+            least = logit_of(low);              // (n = k here)
         }
         const unsigned long long below = (1ull << (threadIdx.x & 63)) - 1;
+        unsigned in = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const bool in = col + j < limit && (equal ? !(v[j] < least) : !(v[j] <= least));
-            const unsigned long long all = __ballot(in);
-            if (in) list[n + __popcll(all & below)] = key_of(v[j], col + j);
+        for (int j = 0; j < 8; ++j) in |= col + j < limit && !(v[j] < bound) && !(v[j] <= least) ? 1u << j : 0u;
+        for (unsigned long long all; (all = __ballot(in != 0)) != 0; in &= in - 1) {                  // (one column of a lane at a time; mostly there is one)
+            const int j = __builtin_ctz(in | 256u);
+            float x = v[0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) x = j == i ? v[i] : x;
+            if (in) list[n + __popcll(all & below)] = key_of(x, col + j);
             n += __popcll(all);
-        }
-    }
-    unsigned limit;                             // columns of the row: what lies past them is no column
-    __device__ void bound_from_list()
-    {
-        const int lane = threadIdx.x & 63;
-        const unsigned o = lane < n ? (unsigned)(list[lane] >> 32) : 0xFFFFFFFFu;
-        unsigned low = o;
-#pragma unroll
-        for (int d = 32; d; d >>= 1) low = min(low, (unsigned)__shfl_xor((int)low, d));
-        if (n >= k) {
-            const float b = logit_of(low);
-            if (!(least >= b)) least = b;
         }
     }
 };
@@ -228,74 +228,91 @@ struct Args {
     Key* keys;
 };
 
+// A given column of a row and its logit, asked for early.
+struct Given {
+    int64_t col;
+    float logit;
+};
 template <class T>
-__device__ inline void finish_row(const Args& a, const T* x, long long row, const Stat& st, Key* list, int n)
+__device__ inline Given given(const Args& a, const T* x, long long row, int j)
 {
-    const int lane = threadIdx.x & 63;
+    Given g = {-1, 0.0f};
+    if (j < a.n_targets) {
+        g.col = a.targets[row * a.n_targets + j];
+        if (g.col >= 0 && g.col < (int64_t)a.cols) g.logit = Elem<T>::get(x[g.col]);
+    }
+    return g;
+}
+
+// What a row's outputs are made of; `lane` of `lanes` threads write them, and in the first wave of those lane i < k has the i-th likeliest.
+template <class T>
+__device__ inline void finish_row(const Args& a, const T* x, long long row, const Stat& st, int lane, int lanes, Given g, Key mine)
+{
     const bool empty = st.m == kLow && st.s == 0.0f;                      // no column above -infinity
     const float ls = logf(st.s);
     const float lse = empty ? -__builtin_inff() : st.m + ls;
     auto log_prob = [&](float v) { return st.s != st.s ? st.s : v == -__builtin_inff() ? v : v - lse; };
-    if (threadIdx.x == 0) {
+    if (lane == 0) {
         a.lse[row] = st.s != st.s ? st.s : lse;
         if (a.entropy) a.entropy[row] = empty ? 0.0f : ls - st.t / st.s;
     }
-    for (int j = threadIdx.x; j < a.n_targets; j += 64 * kWaves) {
-        const int64_t c = a.targets[row * a.n_targets + j];
-        float r = 0.0f;
-        if (c >= (int64_t)a.cols)
-            r = __builtin_nanf("");
-        else if (c >= 0)
-            r = log_prob(Elem<T>::get(x[c]));
-        a.logp[row * a.n_targets + j] = r;
+    for (int j = lane; j < a.n_targets; j += lanes) {
+        if (j >= lanes) g = given(a, x, row, j);
+        a.logp[row * a.n_targets + j] = g.col < 0 ? 0.0f : g.col >= (int64_t)a.cols ? __builtin_nanf("") : log_prob(g.logit);
     }
-    if (a.k && threadIdx.x < 64) {
-        const Key mine = lane < n ? list[lane] : 0;
-        const int place = place_of(mine, n);
-        if (lane < n) {
-            a.top_ids[row * a.k + place] = (int64_t)(unsigned)~(unsigned)mine;
-            a.top_logp[row * a.k + place] = log_prob(logit_of((unsigned)(mine >> 32)));
-        }
+    if (lane < a.k) {
+        a.top_ids[row * a.k + lane] = (int64_t)(unsigned)~(unsigned)mine;
+        a.top_logp[row * a.k + lane] = log_prob(logit_of((unsigned)(mine >> 32)));
     }
 }
 
-// Joins the waves' lists (at most k keys each) to the first one's; all threads call it.
+// The k largest of the waves' lists, in order, in the lists' first k places; all threads call it.  Returns their number.  A list has at most 64 keys by then, so
+// every thread takes one and counts the larger ones.
 __device__ inline int join_lists(Key (*lists)[kHold], int* counts, int n, int k)
 {
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    if (n > 64) n = keep_largest(lists[wave], n, k);
     if (lane == 0) counts[wave] = n;
     __syncthreads();
-    int at = counts[0];
-    if (wave == 0) {
-        for (int w = 1; w < kWaves; ++w) {
-            if (lane < counts[w]) lists[0][at + lane] = lists[w][lane];
-            at += counts[w];
-        }
-        at = keep_largest(lists[0], at, k);
+    const Key mine = lane < n ? lists[wave][lane] : 0;
+    int place = 0, all = 0;
+    for (int w = 0; w < kWaves; ++w) {
+        const int m = counts[w];
+        all += m;
+#pragma unroll 4
+        for (int i = 0; i < m; ++i) place += lists[w][i] > mine;
     }
-    return at;
+    __syncthreads();
+    if (lane < n && place < k) lists[0][place] = mine;
+    __syncthreads();
+    return min(all, k);
 }
 
-// One slice of a row to a workgroup: its waves take steps of 512 columns in turn, so that each sees ascending columns.
-template <class T, bool TOP>
-__global__ __launch_bounds__(64 * kWaves) void score_kernel(const T* __restrict__ logits, const Args a)
+// One slice of a row to a workgroup, whose waves take steps of 512 columns in turn, so that each sees ascending columns; SOLO: a row to a wave.
+template <class T, bool TOP, bool SOLO>
+__global__ __launch_bounds__(64 * kWaves, TOP ? 4 : 1) void score_kernel(const T* __restrict__ logits, const Args a)
 {
     __shared__ Key lists[TOP ? kWaves : 1][TOP ? kHold : 1];
+    __shared__ unsigned tops[TOP && !SOLO ? kWaves : 1][64];
     __shared__ Stat stats[kWaves];
     __shared__ int counts[kWaves];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const long long row = blockIdx.x / (unsigned)a.slices;
-    const unsigned slice = blockIdx.x % (unsigned)a.slices;
+    const long long row = SOLO ? (long long)blockIdx.x * kWaves + wave : blockIdx.x / (unsigned)a.slices;
+    if (SOLO && row >= a.rows) return;
+    const unsigned slice = SOLO ? 0 : blockIdx.x % (unsigned)a.slices;
     const T* const x = logits + row * a.ld;
     const unsigned begin = slice * a.per, end = min(begin + a.per, a.cols);
     constexpr int U = 4;                                                  // steps under way at once
-    constexpr unsigned kTurn = kStep * kWaves;                            // columns of one step of all waves
+    constexpr unsigned kTurn = kStep * (SOLO ? 1 : kWaves);               // columns of one step of all waves
 
+    Given g = {-1, 0.0f};
+    if (a.slices == 1) g = given(a, x, row, SOLO ? lane : (int)threadIdx.x);
     Stat st = {kLow, 0.0f, 0.0f};
     Search find;
-    if constexpr (TOP) find.start(lists[wave], a.k), find.limit = end;
+    if constexpr (TOP) find.start(lists[wave], a.k, end);
     unsigned turn = 0, next_bound = 0;
-    for (unsigned c0 = begin + wave * kStep; c0 < end; c0 += U * kTurn, ++turn) {
+    // (the first turn has a barrier: all waves make it)
+    for (unsigned c0 = begin + (SOLO ? 0 : wave * kStep); c0 < end || (TOP && !SOLO && turn == 0); c0 += U * kTurn, ++turn) {
         Raw<T> raw[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) raw[u] = fetch_unit(x, (c0 + u * kTurn) / 8 + lane, end);
@@ -306,35 +323,65 @@ __global__ __launch_bounds__(64 * kWaves) void score_kernel(const T* __restrict_
             top[u] = add(st, v[u]);
         }
         if constexpr (TOP) {
-            const bool bound = turn == next_bound;                        // at turns 0, 1, 3, 7, ...: the bound rises with the logarithm of what was seen
-            if (bound) next_bound = 2 * turn + 1;
-            if (bound) find.bound(st.s != st.s ? __builtin_nanf("") : st.m == kLow ? -__builtin_inff() : st.m);
+            // A bound at turns 0, 1, 3, 7, ...: it rises with the logarithm of what was seen.  The lanes' largest columns are columns of their own: the k-th largest
+            // among those of all waves is reached by k of the row.  A wave may read what the others saw some turns ago: that is a bound too.
+            if (turn == next_bound) {
+                next_bound = 2 * turn + 1;
+                const unsigned mine = order_of(st.s != st.s ? __builtin_nanf("") : st.m == kLow ? -__builtin_inff() : st.m);
+                if constexpr (SOLO) {
+                    find.raise_bound(kth_of_lanes<1>({mine}, a.k));
+                } else {
+                    __hip_atomic_store(&tops[wave][lane], mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                    if (turn == 0) __syncthreads();
+                    unsigned all[kWaves];
 #pragma unroll
-            for (int u = 0; u < U; ++u) find.show(v[u], top[u], st.s != st.s, c0 + u * kTurn + lane * 8, bound);
+                    for (int w = 0; w < kWaves; ++w) all[w] = __hip_atomic_load(&tops[w][lane], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+                    if (a.k <= 16)                                        // (of 64 lanes' columns few are left out; more alternatives take all 256 lanes')
+                        find.raise_bound(kth_of_lanes<1>({max(max(all[0], all[1]), max(all[2], all[3]))}, a.k));
+                    else
+                        find.raise_bound(kth_of_lanes(all, a.k));
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (c0 + u * kTurn < end) find.show(v[u], top[u], st.s != st.s, c0 + u * kTurn + lane * 8);
         }
     }
     st = wave_join(st);
+    if constexpr (SOLO) {
+        Key mine = 0;
+        if constexpr (TOP) {
+            const int n = find.n > 64 ? keep_largest(find.list, find.n, a.k) : find.n;
+            wave_fence();
+            mine = lane < n ? find.list[lane] : 0;
+            const int place = place_of(mine, n);
+            if (lane < n && place < a.k) find.list[place] = mine;
+            wave_fence();
+            mine = find.list[lane];
+        }
+        finish_row(a, x, row, st, lane, 64, g, mine);
+        return;
+    }
     if (lane == 0) stats[wave] = st;
     int n = 0;
-    if constexpr (TOP) {
-        n = keep_largest(find.list, find.n, a.k);
-        n = join_lists(lists, counts, n, a.k);                            // (its barrier covers stats)
-    } else {
+    if constexpr (TOP)
+        n = join_lists(lists, counts, find.n, a.k);                       // (its barriers cover stats)
+    else
         __syncthreads();
-    }
     st = stats[0];
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) st = join(st, stats[w]);
+    const Key mine = TOP && (int)threadIdx.x < n ? lists[0][threadIdx.x] : 0;
     if (a.slices == 1) {
-        finish_row(a, x, row, st, lists[0], n);
+        finish_row(a, x, row, st, threadIdx.x, 64 * kWaves, g, mine);
     } else {
         if (threadIdx.x == 0) a.parts[blockIdx.x] = {st, (unsigned)n};
         if constexpr (TOP)
-            if (threadIdx.x < n) a.keys[(long long)blockIdx.x * a.k + threadIdx.x] = lists[0][threadIdx.x];
+            if ((int)threadIdx.x < n) a.keys[(long long)blockIdx.x * a.k + threadIdx.x] = mine;
     }
 }
 
-// Joins the slices of a row.
+// Joins the slices of a row.  A slice's keys lie in order; where it has k of them, its k-th is a bound for the row's.
 constexpr int kMaxSlices = 64;
 template <class T, bool TOP>
 __global__ __launch_bounds__(64 * kWaves) void join_kernel(const T* __restrict__ logits, const Args a)
@@ -344,21 +391,43 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(const T* __restrict__
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const long long row = blockIdx.x;
     const Part* const parts = a.parts + row * a.slices;
+    const Key* const keys = a.keys + row * a.slices * a.k;
+    const T* const x = logits + row * a.ld;
+    const Given g = given(a, x, row, threadIdx.x);
     Part p = {{kLow, 0.0f, 0.0f}, 0};
     if (lane < a.slices) p = parts[lane];
+    constexpr int MINE = kMaxSlices / kWaves;                             // slices that a wave looks through: every fourth
+    Key key[TOP ? MINE : 1], least = 0;
+    if constexpr (TOP) {
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) {
+            const int s = i * kWaves + wave;
+            key[i] = s < a.slices && lane < a.k ? keys[s * a.k + lane] : 0;
+        }
+        if (lane < a.slices) least = keys[lane * a.k + a.k - 1];          // (asked for before it is known whether there are k)
+        if ((int)p.n < a.k) least = 0;
+    }
     const Stat st = wave_join(p.st);                                      // (every wave: the same bits)
     int n = 0;
     if constexpr (TOP) {
-        // a wave takes every fourth slice: at most 16 x 64 keys
-        for (int s = wave; s < a.slices; s += kWaves) {
-            const int c = __shfl((int)p.n, s);
-            if (lane < c) lists[wave][n + lane] = a.keys[(row * a.slices + s) * a.k + lane];
-            n += c;
+#pragma unroll
+        for (int d = 32; d; d >>= 1) {
+            const Key other = (Key)(unsigned)__shfl_xor((int)(least >> 32), d) << 32 | (unsigned)__shfl_xor((int)(unsigned)least, d);
+            least = other > least ? other : least;
         }
-        n = keep_largest(lists[wave], n, a.k);
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) {
+            const int s = i * kWaves + wave;
+            if (s >= a.slices) break;
+            const bool in = lane < __shfl((int)p.n, s) && key[i] >= least;
+            const unsigned long long all = __ballot(in);
+            if (in) lists[wave][n + __popcll(all & ((1ull << lane) - 1))] = key[i];
+            n += __popcll(all);
+        }
         n = join_lists(lists, counts, n, a.k);
     }
-    finish_row(a, logits + row * a.ld, row, st, lists[0], n);
+    const Key mine = TOP && (int)threadIdx.x < n ? lists[0][threadIdx.x] : 0;
+    finish_row(a, x, row, st, threadIdx.x, 64 * kWaves, g, mine);
 }
 
 // Slices of a row: enough workgroups to fill the machine, at least 4096 columns each.
@@ -443,6 +512,9 @@ __global__ __launch_bounds__(256) void gradient_kernel(const T* logits, T* grad,
     }
 }
 
+// Rows from which a wave reads a row by itself: nothing to join, and no waves without columns in short rows.  8192 rows, five alternatives, us, a workgroup to a
+// row and so: 1000 columns in 32 bits 51, 18; 4000 in 16 bits 53, 28; 32768 139, 124.  1024 rows of 8000 10, 16: too few waves.
+constexpr long long kSoloRows = 2048;
 constexpr long long kMostGroups = 1ll << 23;                              // workgroups of 256 threads a launch
 
 template <class T>
@@ -460,11 +532,15 @@ int run_scores(const T* logits, Args a, hipStream_t stream)
         if (a.parts) b.parts = a.parts + r0 * a.slices;
         if (a.keys) b.keys = a.keys + r0 * a.slices * a.k;
         const T* const x = logits + r0 * a.ld;
-        const unsigned groups = (unsigned)(b.rows * a.slices);
-        if (a.k)
-            score_kernel<T, true><<<groups, 64 * kWaves, 0, stream>>>(x, b);
+        const unsigned groups = (unsigned)(b.rows * a.slices), solo = (unsigned)((b.rows + kWaves - 1) / kWaves);
+        if (b.rows >= kSoloRows && a.k)
+            score_kernel<T, true, true><<<solo, 64 * kWaves, 0, stream>>>(x, b);
+        else if (b.rows >= kSoloRows)
+            score_kernel<T, false, true><<<solo, 64 * kWaves, 0, stream>>>(x, b);
+        else if (a.k)
+            score_kernel<T, true, false><<<groups, 64 * kWaves, 0, stream>>>(x, b);
         else
-            score_kernel<T, false><<<groups, 64 * kWaves, 0, stream>>>(x, b);
+            score_kernel<T, false, false><<<groups, 64 * kWaves, 0, stream>>>(x, b);
         if (a.slices > 1) {
             if (a.k)
                 join_kernel<T, true><<<(unsigned)b.rows, 64 * kWaves, 0, stream>>>(x, b);

@@ -71,6 +71,17 @@ def test_against_64_bits(dtype, rows, cols, pad, n, k):
     _compare(_logits(rows + cols, rows, cols, dtype, pad), _targets(cols, rows, cols, n), k)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols,pad,n,k,masked", [(2049, 5, 0, 1, 5, 0.3), (2050, 700, 1, 2, 20, 0.0), (2051, 2050, 0, 1, 64, 0.5), (2048, 5001, 3, 70, 1, 0.98), (2048, 513, 0, 1, 0, 0.0)])
+def test_many_rows(dtype, rows, cols, pad, n, k, masked):
+    x = _logits(rows + cols, rows, cols, dtype, pad, masked)
+    x[7] = -INF
+    x[9, cols // 2] = float("nan")
+    x[11] = torch.arange(cols, device="cuda") * 0.01
+    x[13] = 2.0
+    _compare(x, _targets(cols, rows, cols, n), k)
+
+
 @pytest.mark.parametrize("cols", [100, 5000, 40000])
 @pytest.mark.parametrize("k", [1, 17, 64])
 @pytest.mark.parametrize("kind", ["ascending", "descending", "equal", "zeros", "two values", "one", "few", "none", "low", "steps"])
