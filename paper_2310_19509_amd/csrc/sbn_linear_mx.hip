@@ -71,6 +71,9 @@ struct LinearArgs {
     int c_out, blocks, steps, quads, tile_rows, act;
 };
 
+// A value that all lanes of a wave agree on, as a scalar.
+__device__ inline unsigned uniform(unsigned v) { return (unsigned)__builtin_amdgcn_readfirstlane((int)v); }
+
 // The scale a byte stands for, as the conversions take it: 255 is NaN.
 __device__ inline float mx_scale(unsigned byte)
 {
@@ -139,14 +142,14 @@ __device__ inline void finish4(const LinearArgs& a, long long row, int n, f4 v)
 
 enum { kNarrow, kScaled8, kWide8 };         // 4-bit rows; 8-bit rows on scaled multiplies; 8-bit rows as bfloat16
 
-// Few rows: 16 RT rows x 16 NT output channels to a workgroup, whose WAVES waves take the quads of steps (512 input channels) in turn and
-// join their sums in LDS.  Bound by reading the weights once, which go from memory to registers in one 16-byte load per lane and
+// Few rows: 16 RT rows x 16 NT output channels to a workgroup, whose WAVES waves take the quads of steps (512 input channels; halves or quarters of them where
+// there are fewer quads than waves) in turn and join their sums in LDS.  Bound by reading the weights once, which go from memory to registers in one 16-byte load per lane and
 // step; the rows, read again by every workgroup, come from L2.
 template <int MODE, bool BLOCKS, class T, int NT, int RT, int WAVES>
 __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(const LinearArgs a)
 {
     __shared__ f4 sums[WAVES][NT * RT][64];
-    const int wave = (int)threadIdx.x >> 6, lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+    const int wave = (int)uniform(threadIdx.x >> 6), lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
     const int tile0 = blockIdx.x * NT;
     const long long row0 = (long long)blockIdx.y * (16 * RT);
     constexpr int BB = MODE == kNarrow ? 16 : 32;                         // bytes of a block of a row
@@ -160,7 +163,10 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(const LinearArgs a
         xs[j] = a.xs + (live[j] ? row : row0) * a.blocks;
     }
     f4 acc[NT][RT] = {};
-    for (int q = wave; q < a.quads; q += WAVES) {
+    const int parts = a.quads >= WAVES ? 1 : a.quads >= WAVES / 2 ? 2 : 4;
+    for (int p = wave; p < a.quads * parts; p += WAVES) {
+        const int q = p / parts, from = p % parts * (4 / parts), to = from + 4 / parts;
+        const auto mine = [&](int s) { return s >= from && s < to; };
         unsigned ws[NT], sx[RT];
         u4 w[NT][4];
 #pragma unroll
@@ -168,7 +174,8 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(const LinearArgs a
             const long long tile = min(tile0 + t, a.tile_rows - 1);
             ws[t] = ((const unsigned*)a.ws)[(tile * a.quads + q) * 64 + lane];
 #pragma unroll
-            for (int s = 0; s < 4; ++s) w[t][s] = ((const u4*)a.w)[(tile * a.steps + min(q * 4 + s, a.steps - 1)) * 64 + lane];     // (past c_in: the scale is 0)
+            for (int s = 0; s < 4; ++s)
+                if (mine(s)) w[t][s] = ((const u4*)a.w)[(tile * a.steps + min(q * 4 + s, a.steps - 1)) * 64 + lane];     // (past c_in: the scale is 0)
         }
 #pragma unroll
         for (int j = 0; j < RT; ++j) {
@@ -192,6 +199,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_rows_kernel(const LinearArgs a
         }
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
+            if (!mine(s)) continue;
             if constexpr (MODE == kWide8) {
                 b8 B[RT][4];
                 const int block = (q * 4 + s) * 4 + g;
@@ -253,7 +261,6 @@ __device__ inline void load_to_lds(u4 buffer, unsigned offset, unsigned scalar_o
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "s"(lds), "v"(offset), "s"(buffer), "s"(scalar_offset) : "memory", "m0");
 }
-__device__ inline unsigned uniform(unsigned v) { return (unsigned)__builtin_amdgcn_readfirstlane((int)v); }
 
 // Tiles: CH = 16 MT WN output channels x RW = 16 NT WM rows to a workgroup of WN x WM waves, each 16 MT x 16 NT.
 //
@@ -513,12 +520,12 @@ void launch_tiles(const LinearArgs& a, hipStream_t stream)
     tile_kernel<MODE, FMT != SBN_FP8_ROW, T, MT, NT, WN, WM><<<(tn * tm + 7) / 8 * 8, 64 * WN * WM, 0, stream>>>(a, tn, tm);
 }
 
-template <int FMT, class T, int NT, int RT>
+template <int FMT, class T, int NT, int RT, int WAVES>
 void launch_few(const LinearArgs& a, hipStream_t stream)
 {
     constexpr int MODE = FMT == SBN_MXFP4 ? kNarrow : sizeof(T) == 4 ? kWide8 : kScaled8;
     const dim3 grid((unsigned)((a.tile_rows + NT - 1) / NT), (unsigned)((a.rows + 16 * RT - 1) / (16 * RT)));
-    few_rows_kernel<MODE, FMT != SBN_FP8_ROW, T, NT, RT, 4><<<grid, 256, 0, stream>>>(a);
+    few_rows_kernel<MODE, FMT != SBN_FP8_ROW, T, NT, RT, WAVES><<<grid, 64 * WAVES, 0, stream>>>(a);
 }
 
 // Which kernel, by what each takes, in microseconds, measured with both over 32 to 8192 rows and 1000 to 32768 channels.
@@ -568,9 +575,9 @@ int run_linear(LinearArgs a, int cus, hipStream_t stream)
             if constexpr (MODE == kScaled8) launch_tiles<FMT, T, 4, 8, 4, 2>(b, stream);
             break;
         case 44: launch_tiles<FMT, T, 4, 4, 2, 2>(b, stream); break;
-        case 22: launch_few<FMT, T, 2, 2>(b, stream); break;
-        case 21: launch_few<FMT, T, 2, 1>(b, stream); break;
-        default: launch_few<FMT, T, 1, 1>(b, stream); break;
+        case 22: launch_few<FMT, T, 2, 2, 4>(b, stream); break;
+        case 21: launch_few<FMT, T, 2, 1, 4>(b, stream); break;
+        default: launch_few<FMT, T, 1, 1, 8>(b, stream); break;
         }
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return fail(SBN_EHIP, "sbn_linear_mx: %s", hipGetErrorString(e));
     }

@@ -336,7 +336,7 @@ __global__ __launch_bounds__(64 * kWaves, TOP ? 4 : 1) void score_kernel(const T
                     unsigned all[kWaves];
 #pragma unroll
                     for (int w = 0; w < kWaves; ++w) all[w] = __hip_atomic_load(&tops[w][lane], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
-                    if (a.k <= 16)                                        // (of 64 lanes' columns few are left out; more alternatives take all 256 lanes')
+                    if (a.k <= 32)                                        // (of 64 lanes' columns few are left out; more alternatives take all 256 lanes')
                         find.raise_bound(kth_of_lanes<1>({max(max(all[0], all[1]), max(all[2], all[3]))}, a.k));
                     else
                         find.raise_bound(kth_of_lanes(all, a.k));
@@ -419,7 +419,7 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(const T* __restrict__
         for (int i = 0; i < MINE; ++i) {
             const int s = i * kWaves + wave;
             if (s >= a.slices) break;
-            const bool in = lane < __shfl((int)p.n, s) && key[i] >= least;
+            const bool in = lane < __builtin_amdgcn_readlane((int)p.n, s) && key[i] >= least;
             const unsigned long long all = __ballot(in);
             if (in) lists[wave][n + __popcll(all & ((1ull << lane) - 1))] = key[i];
             n += __popcll(all);
@@ -430,11 +430,11 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(const T* __restrict__
     finish_row(a, x, row, st, threadIdx.x, 64 * kWaves, g, mine);
 }
 
-// Slices of a row: enough workgroups to fill the machine, at least 4096 columns each.
+// Slices of a row: enough workgroups to fill the machine, at least 8192 columns each, which is one turn of a workgroup.
 int slices_of(long long rows, long long cols)
 {
     constexpr long long kWorkgroups = 1024;
-    const long long by_work = cols / 4096, by_rows = rows >= kWorkgroups ? 1 : kWorkgroups / std::max(rows, 1ll);
+    const long long by_work = cols / 8192, by_rows = rows >= kWorkgroups ? 1 : kWorkgroups / std::max(rows, 1ll);
     return (int)std::max(1ll, std::min({by_work, by_rows, (long long)kMaxSlices}));
 }
 

@@ -213,6 +213,10 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void row_kernel(cons
         rx[i] = fetch_unit(x, i * THREADS + t, cols);
         if constexpr (ADD) rr[i] = fetch_unit(res, i * THREADS + t, cols);
     }
+    // Few rows wait for memory: their weights are asked for together with the rows.
+    constexpr bool EARLY = ITEMS == 1;
+    Raw<float> rw = {};
+    if (EARLY && a.weight) rw = fetch_unit(a.weight, t, cols);
     float v[ITEMS][8];
     float sum = 0.0f;
 #pragma unroll
@@ -236,7 +240,7 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void row_kernel(cons
             const int unit = i * THREADS + t;
             float w[8];
             if (a.weight) {
-                expand_unit(fetch_unit(a.weight, unit, cols), a.weight, unit, cols, w, 0.0f);
+                expand_unit(EARLY ? rw : fetch_unit(a.weight, unit, cols), a.weight, unit, cols, w, 0.0f);
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) w[j] = 1.0f;
