@@ -1,0 +1,90 @@
+"""Scores tokens with a small language model's last layers, all of its weights in microscaled 4 bits.
+
+Every block adds its input to the residual stream, normalises it into 8-bit rows and takes them through two layers with a
+ReLU between; the head normalises once more, multiplies with the vocabulary and reports the log probability of the
+token that came, the entropy and the likeliest alternatives:
+
+    sbn_add_rmsnorm -> sbn_linear_mx (ReLU) -> sbn_quantize -> sbn_linear_mx -> ...  -> sbn_add_rmsnorm -> sbn_linear_mx -> sbn_log_probs
+
+Weights are random (there is no checkpoint here); the first layers' may be block-pruned as the sparse layers' are.
+
+    python examples/scoring_head.py --rows 512 --hidden 1024 --blocks 4 --vocab 32000
+"""
+import argparse
+import os
+import sys
+import time
+
+import numpy as np
+import torch
+
+sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+import paper_2310_19509_amd as S  # noqa: E402
+
+
+class ScoringHead:
+    """Packed layers, norm weights and the buffers for up to `rows` rows; everything is allocated here, run() only launches."""
+
+    def __init__(self, rows, hidden, blocks, vocab, top=5, fmt=S.SBN_MXFP8, sparsity=0, seed=0):
+        rng = np.random.default_rng(seed)
+        self.fmt, self.top, self.hidden, self.vocab = fmt, top, hidden, vocab
+        self.weights = []                       # what was packed, for whoever checks the results: (w, mask)
+
+        def layer(n, k, act=S.SBN_ACT_NONE):
+            w = (rng.standard_normal((n, 1, 1, k)) / np.sqrt(k)).astype(np.float32)
+            mask = S.sbn_prune_magnitude(w, S.SBN_CONV1X1, 4, 4, sparsity) if sparsity and act else None
+            self.weights.append((w, mask))
+            return S.sbn_mx_pack(w, mask=mask, act=act)
+
+        self.blocks = [(layer(4 * hidden, hidden, S.SBN_ACT_RELU), layer(hidden, 4 * hidden)) for _ in range(blocks)]
+        self.head = layer(vocab, hidden)
+        self.norms = [torch.from_numpy((1 + 0.1 * rng.standard_normal(hidden)).astype(np.float32)).cuda() for _ in range(blocks + 1)]
+        new = lambda *s, dtype=torch.bfloat16: torch.empty(s, dtype=dtype, device="cuda")  # noqa: E731
+        self.narrow, self.wide = S.sbn_quantized_empty(fmt, rows, hidden), S.sbn_quantized_empty(fmt, rows, 4 * hidden)
+        self.up, self.down, self.logits = new(rows, 4 * hidden), new(rows, hidden), new(rows, vocab)
+        f32 = torch.float32
+        self.logp, self.lse, self.entropy = new(rows, 1, dtype=f32), new(rows, dtype=f32), new(rows, dtype=f32)
+        self.ids, self.top_logp = new(rows, top, dtype=torch.int64), new(rows, top, dtype=f32)
+        sizes = [S.sbn_linear_mx_workspace(p, fmt, rows) for b in self.blocks for p in b] + [S.sbn_linear_mx_workspace(self.head, fmt, rows), S.sbn_log_probs_workspace(rows, vocab, top)]
+        self.workspace = torch.empty(max(max(sizes), 16), dtype=torch.uint8, device="cuda")
+
+    def run(self, x, residual, targets):
+        """x, residual [rows][hidden] in bfloat16 (the residual is updated), targets int64 [rows][1]."""
+        ws = self.workspace
+        for (up, down), weight in zip(self.blocks, self.norms):
+            S.sbn_add_rmsnorm(x, weight, 1e-6, residual=residual, total=residual, fmt=self.fmt, codes=self.narrow[0], scales=self.narrow[1])
+            S.sbn_linear_mx(up, *self.narrow, self.fmt, self.up, workspace=ws)
+            S.sbn_quantize(self.up, self.fmt, *self.wide)
+            S.sbn_linear_mx(down, *self.wide, self.fmt, self.down, workspace=ws)
+            x = self.down
+        S.sbn_add_rmsnorm(x, self.norms[-1], 1e-6, residual=residual, total=residual, fmt=self.fmt, codes=self.narrow[0], scales=self.narrow[1])
+        S.sbn_linear_mx(self.head, *self.narrow, self.fmt, self.logits, workspace=ws)
+        S.sbn_log_probs(self.logits, targets, self.top, self.logp, self.lse, self.entropy, self.ids, self.top_logp, workspace=ws)
+        return self.logp, self.entropy, self.ids, self.top_logp
+
+
+def main():
+    p = argparse.ArgumentParser(description=__doc__.split("\n")[0])
+    for name, value in (("rows", 512), ("hidden", 1024), ("blocks", 4), ("vocab", 32000), ("top", 5), ("sparsity", 0), ("passes", 50)):
+        p.add_argument("--" + name, type=int, default=value)
+    a = p.parse_args()
+    head = ScoringHead(a.rows, a.hidden, a.blocks, a.vocab, a.top, sparsity=a.sparsity)
+    x, start = (torch.randn(a.rows, a.hidden, device="cuda").bfloat16() for _ in range(2))
+    targets = torch.randint(0, a.vocab, (a.rows, 1), device="cuda")
+    residual = start.clone()
+    logp, entropy, ids, top = head.run(x, residual, targets)
+    print(f"mean log probability {float(logp.mean()):.4f}, mean entropy {float(entropy.mean()):.4f} (uniform: {np.log(a.vocab):.4f})")
+    print("first row's alternatives:", ", ".join(f"{i} ({v:.3f})" for i, v in zip(ids[0].tolist(), top[0].tolist())))
+    torch.cuda.synchronize()
+    t = time.perf_counter()
+    for _ in range(a.passes):
+        residual.copy_(start)
+        head.run(x, residual, targets)
+    torch.cuda.synchronize()
+    t = (time.perf_counter() - t) / a.passes
+    held = sum(S.sbn_mx_info(l)["device_bytes"] for b in head.blocks for l in b) + S.sbn_mx_info(head.head)["device_bytes"]
+    print(f"{a.rows} rows in {t * 1e6:.0f} us ({a.rows / t:.0f} tokens/s), {held / 2 ** 20:.1f} MiB of weights")
+
+
+if __name__ == "__main__":
+    main()
