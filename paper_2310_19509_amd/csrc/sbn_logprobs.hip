@@ -289,7 +289,7 @@ __device__ inline int join_lists(Key (*lists)[kHold], int* counts, int n, int k)
 }
 
 // One slice of a row to a workgroup, whose waves take steps of 512 columns in turn, so that each sees ascending columns; SOLO: a row to a wave.
-template <class T, bool TOP, bool SOLO>
+template <class T, bool TOP, bool SOLO, bool ONCE>
 __global__ __launch_bounds__(64 * kWaves, TOP ? 4 : 1) void score_kernel(const T* __restrict__ logits, const Args a)
 {
     __shared__ Key lists[TOP ? kWaves : 1][TOP ? kHold : 1];
@@ -315,7 +315,7 @@ __global__ __launch_bounds__(64 * kWaves, TOP ? 4 : 1) void score_kernel(const T
     for (unsigned c0 = begin + (SOLO ? 0 : wave * kStep); c0 < end || (TOP && !SOLO && turn == 0); c0 += U * kTurn, ++turn) {
         Raw<T> raw[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) raw[u] = fetch_unit(x, (c0 + u * kTurn) / 8 + lane, end);
+        for (int u = 0; u < U; ++u) raw[u] = fetch_unit<ONCE>(x, (c0 + u * kTurn) / 8 + lane, end);
         float v[U][8], top[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -449,7 +449,7 @@ struct BackArgs {
 // dx = - p (G + g_H (log p + H)), plus g_j at target j.  Bound by reading the logits and writing the gradient; a lane holds the
 // targets of eight columns only if one of them falls there, which is looked up in LDS per unit for up to kTargets at a time.
 constexpr int kTargets = 64;
-template <class T>
+template <class T, bool ONCE>
 __global__ __launch_bounds__(256) void gradient_kernel(const T* logits, T* grad, const BackArgs a)
 {
     __shared__ float lds_g[kTargets];
@@ -480,7 +480,7 @@ __global__ __launch_bounds__(256) void gradient_kernel(const T* logits, T* grad,
     for (unsigned c0 = begin + threadIdx.x * 8; c0 < end; c0 += U * 2048) {
         Raw<T> raw[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) raw[u] = fetch_unit(x, (c0 + u * 2048) / 8, end);
+        for (int u = 0; u < U; ++u) raw[u] = fetch_unit<ONCE>(x, (c0 + u * 2048) / 8, end);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const unsigned c = c0 + u * 2048;
@@ -533,14 +533,16 @@ int run_scores(const T* logits, Args a, hipStream_t stream)
         if (a.keys) b.keys = a.keys + r0 * a.slices * a.k;
         const T* const x = logits + r0 * a.ld;
         const unsigned groups = (unsigned)(b.rows * a.slices), solo = (unsigned)((b.rows + kWaves - 1) / kWaves);
+        constexpr bool MAY = sizeof(T) == 2;
+        const bool once = read_once<T>(all, a.cols);
         if (b.rows >= kSoloRows && a.k)
-            score_kernel<T, true, true><<<solo, 64 * kWaves, 0, stream>>>(x, b);
+            (once ? score_kernel<T, true, true, MAY> : score_kernel<T, true, true, false>)<<<solo, 64 * kWaves, 0, stream>>>(x, b);
         else if (b.rows >= kSoloRows)
-            score_kernel<T, false, true><<<solo, 64 * kWaves, 0, stream>>>(x, b);
+            (once ? score_kernel<T, false, true, MAY> : score_kernel<T, false, true, false>)<<<solo, 64 * kWaves, 0, stream>>>(x, b);
         else if (a.k)
-            score_kernel<T, true, false><<<groups, 64 * kWaves, 0, stream>>>(x, b);
+            (once ? score_kernel<T, true, false, MAY> : score_kernel<T, true, false, false>)<<<groups, 64 * kWaves, 0, stream>>>(x, b);
         else
-            score_kernel<T, false, false><<<groups, 64 * kWaves, 0, stream>>>(x, b);
+            (once ? score_kernel<T, false, false, MAY> : score_kernel<T, false, false, false>)<<<groups, 64 * kWaves, 0, stream>>>(x, b);
         if (a.slices > 1) {
             if (a.k)
                 join_kernel<T, true><<<(unsigned)b.rows, 64 * kWaves, 0, stream>>>(x, b);
@@ -562,7 +564,8 @@ int run_gradient(const T* logits, T* grad, long long rows, BackArgs a, hipStream
         BackArgs b = a;
         b.targets = a.targets + r0 * a.n_targets, b.g_logp = a.g_logp + r0 * a.n_targets, b.lse = a.lse + r0;
         if (a.g_entropy) b.entropy = a.entropy + r0, b.g_entropy = a.g_entropy + r0;
-        gradient_kernel<T><<<(unsigned)(std::min(most, rows - r0) * a.slices), 256, 0, stream>>>(logits + r0 * a.ld, grad + r0 * a.ldg, b);
+        auto* const kernel = read_once<T>(rows, a.cols) ? gradient_kernel<T, sizeof(T) == 2> : gradient_kernel<T, false>;
+        kernel<<<(unsigned)(std::min(most, rows - r0) * a.slices), 256, 0, stream>>>(logits + r0 * a.ld, grad + r0 * a.ldg, b);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return fail(SBN_EHIP, "sbn_log_probs_backward: %s", hipGetErrorString(e));
     }
     return SBN_OK;

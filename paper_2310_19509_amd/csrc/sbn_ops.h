@@ -12,6 +12,17 @@ constexpr int kEmax4 = 2, kEmax8 = 8;
 constexpr float kTop8 = 448.0f;
 constexpr float kLeastRow = 6.018531e-36f;            // 2^-117: below it 448 / a leaves 32 bits
 
+// Rows of 16-bit elements from this size on cannot have stayed in the last level of cache (256 MB) whole since they were written; kernels that read them
+// once then say so with every load.  us without and with: 8192 x 8192 to 4 bits and back 65, 57; the same to rows of 8 bits 69, 64; scores and gradient of
+// 4096 x 32768 168, 160, of 8192 x 32768 327, 302.  Smaller ones are slower so when they come out of the cache (norm of 1021 x 5001 13.7, 16.2), and so are
+// 32-bit rows, whose lanes take 32 bytes in two loads of half a sector each (4096 x 8192 norm 87, 89).
+constexpr long long kOnceBytes = 128ll << 20;
+template <class T>
+inline bool read_once(long long rows, long long cols)
+{
+    return sizeof(T) == 2 && rows * cols * 2 >= kOnceBytes;
+}
+
 #ifdef __HIPCC__
 
 typedef float f4 __attribute__((ext_vector_type(4)));
@@ -46,12 +57,14 @@ template <> struct Elem<_Float16> {
 template <class T> struct Raw {
     u4 w[sizeof(T) / 2];
 };
-template <class T>
+// ONCE: read for the only time and marked so in the caches, which leaves them to what the call writes (see kOnceBytes).
+typedef u4 u4_any __attribute__((aligned(2)));
+template <bool ONCE, class T>
 __device__ inline Raw<T> fetch(const T* p)
 {
     Raw<T> r;
 #pragma unroll
-    for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = ((const Any16*)p)[i].v;
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = ONCE ? __builtin_nontemporal_load((const u4_any*)p + i) : ((const u4_any*)p)[i];
     return r;
 }
 __device__ inline void expand(const Raw<float>& r, float (&v)[8])
@@ -80,10 +93,10 @@ __device__ inline void expand(const Raw<_Float16>& r, float (&v)[8])
 // Columns 8 unit .. + 7 of a row, in two steps so that several loads are under way before the first is used: all lanes
 // load eight elements (those past the row's end its last eight, when it has as many), and the lanes at the end
 // correct what they have.
-template <class T>
+template <bool ONCE = false, class T>
 __device__ inline Raw<T> fetch_unit(const T* row, long long unit, long long cols)
 {
-    return cols >= 8 ? fetch(row + min(unit * 8, cols - 8)) : Raw<T>{};
+    return cols >= 8 ? fetch<ONCE>(row + min(unit * 8, cols - 8)) : Raw<T>{};
 }
 template <class T>
 __device__ inline void expand_unit(const Raw<T>& r, const T* row, long long unit, long long cols, float (&v)[8], float rest)

@@ -30,7 +30,7 @@ __device__ inline void put_block_codes(const float (&v)[8], void* codes, uint8_t
 
 // Blocks.  A thread takes kItems units of the launch's rows, a workgroup apart.
 constexpr int kItems = 4;
-template <class T, int FMT>
+template <class T, int FMT, bool ONCE>
 __global__ __launch_bounds__(256) void quantize_kernel(const T* __restrict__ x, long long ldx, unsigned units, unsigned total,
                                                        long long cols, void* __restrict__ codes, uint8_t* __restrict__ scales)
 {
@@ -43,7 +43,7 @@ __global__ __launch_bounds__(256) void quantize_kernel(const T* __restrict__ x, 
         const unsigned u = min(first + 256u * i, total - 1u);
         row[i] = x + (long long)(u / units) * ldx;
         unit[i] = u % units;
-        raw[i] = fetch_unit(row[i], unit[i], cols);
+        raw[i] = fetch_unit<ONCE>(row[i], unit[i], cols);
     }
 #pragma unroll
     for (int i = 0; i < kItems; ++i) {
@@ -191,7 +191,7 @@ __device__ inline float row_scale(unsigned top, float& inverse)
 }
 
 // One row to THREADS threads, held in registers: ITEMS units each.  RT: the residual's type, or void.
-template <class XT, class RT, int THREADS, int ITEMS>
+template <class XT, class RT, int THREADS, int ITEMS, bool ONCE = false>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void row_kernel(const RowArgs a)
 {
     __shared__ float lds_sum[16];
@@ -210,8 +210,8 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void row_kernel(cons
     Raw<R> rr[ITEMS];
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
-        rx[i] = fetch_unit(x, i * THREADS + t, cols);
-        if constexpr (ADD) rr[i] = fetch_unit(res, i * THREADS + t, cols);
+        rx[i] = fetch_unit<ONCE>(x, i * THREADS + t, cols);
+        if constexpr (ADD) rr[i] = fetch_unit<ONCE>(res, i * THREADS + t, cols);
     }
     // Few rows wait for memory: their weights are asked for together with the rows.
     constexpr bool EARLY = ITEMS == 1;
@@ -344,16 +344,18 @@ int launch_rows(RowArgs a, hipStream_t stream)
         if (a.y) b.y = (XT*)a.y + r0 * a.ldy;
         if (fmt) b.codes = (char*)a.codes + r0 * per, b.scales = (char*)a.scales + r0 * (fmt == SBN_FP8_ROW ? 4 : units / 4);
         const unsigned rows = (unsigned)b.rows;
+        constexpr bool MAY = sizeof(XT) == 2;
+        const bool once = read_once<XT>(a.rows, a.cols);
         if (units <= 256 && rows >= 1024)
-            row_kernel<XT, RT, 64, 4><<<(rows + 3) / 4, 256, 0, stream>>>(b);
+            (once ? row_kernel<XT, RT, 64, 4, MAY> : row_kernel<XT, RT, 64, 4>)<<<(rows + 3) / 4, 256, 0, stream>>>(b);
         else if (units <= 512)
-            row_kernel<XT, RT, 256, 2><<<rows, 256, 0, stream>>>(b);
+            (once ? row_kernel<XT, RT, 256, 2, MAY> : row_kernel<XT, RT, 256, 2>)<<<rows, 256, 0, stream>>>(b);
         else if (units <= 1024 && rows >= 512)
-            row_kernel<XT, RT, 256, 4><<<rows, 256, 0, stream>>>(b);
+            (once ? row_kernel<XT, RT, 256, 4, MAY> : row_kernel<XT, RT, 256, 4>)<<<rows, 256, 0, stream>>>(b);
         else if (units <= 1024)
             row_kernel<XT, RT, 1024, 1><<<rows, 1024, 0, stream>>>(b);
         else if (units <= 4096)
-            row_kernel<XT, RT, 1024, 4><<<rows, 1024, 0, stream>>>(b);
+            (once ? row_kernel<XT, RT, 1024, 4, MAY> : row_kernel<XT, RT, 1024, 4>)<<<rows, 1024, 0, stream>>>(b);
         else
             long_row_kernel<XT, RT><<<rows, 1024, 0, stream>>>(b);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return fail(SBN_EHIP, "row kernel: %s", hipGetErrorString(e));
@@ -381,10 +383,12 @@ int quantize_blocks(const T* x, long long rows, long long cols, long long ldx, i
     return by_rows(rows, units, "sbn_quantize", [&](long long n, long long r0) {
         const unsigned total = (unsigned)(n * units);
         uint8_t* const s = (uint8_t*)scales + r0 * (units / 4);
-        if (format == SBN_MXFP4)
-            quantize_kernel<T, SBN_MXFP4><<<groups_of(total), 256, 0, stream>>>(x + r0 * ldx, ldx, (unsigned)units, total, cols, codes + r0 * units * 4, s);
-        else
-            quantize_kernel<T, SBN_MXFP8><<<groups_of(total), 256, 0, stream>>>(x + r0 * ldx, ldx, (unsigned)units, total, cols, codes + r0 * units * 8, s);
+        char* const c = codes + r0 * units * (format == SBN_MXFP4 ? 4 : 8);
+        constexpr bool MAY = sizeof(T) == 2;
+        const bool once = read_once<T>(rows, cols);
+        auto* const kernel = format == SBN_MXFP4 ? (once ? quantize_kernel<T, SBN_MXFP4, MAY> : quantize_kernel<T, SBN_MXFP4, false>)
+                                                 : (once ? quantize_kernel<T, SBN_MXFP8, MAY> : quantize_kernel<T, SBN_MXFP8, false>);
+        kernel<<<groups_of(total), 256, 0, stream>>>(x + r0 * ldx, ldx, (unsigned)units, total, cols, c, s);
     });
 }
 
