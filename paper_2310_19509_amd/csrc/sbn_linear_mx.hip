@@ -528,29 +528,47 @@ void launch_few(const LinearArgs& a, hipStream_t stream)
     few_rows_kernel<MODE, FMT != SBN_FP8_ROW, T, NT, RT, WAVES><<<grid, 64 * WAVES, 0, stream>>>(a);
 }
 
-// Which kernel, by what each takes, in microseconds, measured with both over 32 to 8192 rows and 1000 to 32768 channels.
+// Which kernel, by what each takes, in microseconds, fitted to 15 shapes (256 to 8192 rows, 512 to 8192 input and 1024 to 14336 output channels)
+// and within a tenth of nearly all of them:
 //   few rows (16 or 32 of them to a workgroup): the weights once more for every 32 rows: 3 + operations / rate, the rate 750, 470
 //     or 500 TFLOP/s (4-bit rows, 8-bit rows, 8-bit rows to 32 bits).  Of 16 rows at most nothing else comes near:
 //     8192 -> 32768 channels, 16 rows in 8 bits: 29 us, 42 in tiles.
-//   tiles of 128 x 128: 2 + 0.36, 0.5 or 1 per 128 input channels for as many tiles as there are compute units.
-//   tiles of 256 x 256: 8/3 of a round of those, for four times the work: 8192^3 in 4 bits 255 us, 345 in the small ones; 2048 x 4096 x 4096, half
-//     a round, 32 us and 25.  Not for 32-bit results of 8-bit rows, where the conversions to bfloat16 leave no registers.
+//   tiles: 3, and so much plus so much per 128 input channels for every two tiles a compute unit, which it has at work at a time, and
+//     for a last one that it works on alone.  (256 rows x 256 channels leave no room for two.)  On three shapes, in 4 bits:
+//                                128 x 128   128 rows x 256   256 x 256
+//        1024 x 4096 x  4096       16 us          19              30
+//        2048 x 4096 x 11000       65             53              67
+//        8192 x 8192 x  8192      339            260             248
+//     Rows in 8 bits: 256 x 256 are never the best, 8192^3 in 473, 377 and 387.  32-bit results of them: 128 x 128 alone, as the
+//     conversions to bfloat16 leave no registers for more (128 x 256: 142 us of 4096^3, 114).
+struct TileCost {
+    int form, rows, channels;
+    double two, two_step, one, one_step;
+};
+constexpr TileCost kTileCosts[3][3] = {
+    {{44, 128, 128, 2.5, 0.61, 0, 0.38}, {84, 128, 256, 4, 0.92, 1, 0.56}, {164, 256, 256, 12, 1.74, 6, 0.87}},     // kNarrow
+    {{44, 128, 128, 2.5, 0.87, 0, 0.60}, {84, 128, 256, 4, 1.38, 2, 0.84}},                                          // kScaled8
+    {{44, 128, 128, 2.5, 1.70, 0, 1.07}},                                                                            // kWide8
+};
 int form_for(const LinearArgs& a, int mode, int cus)
 {
     const int forced = forced_kernel_form(SBN_LINEAR_MX);
-    const auto groups = [&](int side) { return ((long long)a.c_out + side - 1) / side * ((a.rows + side - 1) / side); };
-    const auto rounds = [&](int side) { return (groups(side) + cus - 1) / cus; };
     // a tile of rows has to lie within 31 bits, the scales to fill a load
     const bool tiles = (long long)a.blocks * 32 * 256 < 1ll << 31 && a.rows * a.blocks >= 16;
-    const int wide = mode == kNarrow ? 164 : mode == kScaled8 ? 88 : 44, few = a.rows > 16 ? 22 : a.tile_rows >= 2 * cus ? 21 : 11;
+    const int few = a.rows > 16 ? 22 : a.tile_rows >= 2 * cus ? 21 : 11;
     if (forced == 11 || forced == 21 || forced == 22) return forced;
-    if (forced) return !tiles ? few : forced == 44 ? 44 : wide;
-    if (!tiles || a.rows <= 16) return few;
-    const double rate[] = {750e6, 470e6, 500e6}, step[] = {0.36, 0.5, 1.0};
-    const double by_few = 3.0 + 2.0 * (double)((a.rows + 31) / 32 * 32) * a.c_out * a.steps * 128.0 / rate[mode];
-    const double by_tiles = (double)rounds(128) * (2.0 + step[mode] * a.steps);
-    if (by_few <= by_tiles) return few;
-    return 8 * rounds(256) <= 3 * rounds(128) ? wide : 44;
+    if (!tiles || (!forced && a.rows <= 16)) return few;
+    if (forced) return mode == kWide8 || forced == 44 ? 44 : mode == kScaled8 || forced == 84 ? 84 : 164;
+    const double rate[] = {750e6, 470e6, 500e6};
+    double least = 3.0 + 2.0 * (double)((a.rows + 31) / 32 * 32) * a.c_out * a.steps * 128.0 / rate[mode];
+    int form = few;
+    for (const TileCost& c : kTileCosts[mode]) {
+        if (!c.form) break;
+        const long long groups = ((long long)a.c_out + c.channels - 1) / c.channels * ((a.rows + c.rows - 1) / c.rows), rounds = (groups + cus - 1) / cus;
+        const double cost = 3.0 + (double)(rounds / 2) * (c.two + c.two_step * a.steps) + (double)(rounds % 2) * (c.one + c.one_step * a.steps);
+        if (cost < least) least = cost, form = c.form;
+    }
+    return form;
 }
 
 template <int FMT, class T>
@@ -571,8 +589,8 @@ int run_linear(LinearArgs a, int cus, hipStream_t stream)
         case 164:
             if constexpr (MODE == kNarrow) launch_tiles<FMT, T, 4, 16, 4, 1>(b, stream);
             break;
-        case 88:
-            if constexpr (MODE == kScaled8) launch_tiles<FMT, T, 4, 8, 4, 2>(b, stream);
+        case 84:
+            if constexpr (MODE != kWide8) launch_tiles<FMT, T, 4, 8, 4, 1>(b, stream);
             break;
         case 44: launch_tiles<FMT, T, 4, 4, 2, 2>(b, stream); break;
         case 22: launch_few<FMT, T, 2, 2, 4>(b, stream); break;

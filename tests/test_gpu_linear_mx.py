@@ -73,7 +73,7 @@ def test_against_64_bits(fmt, dtype, rows, k, n, bias, act):
     assert torch.equal(y, _run(p, codes, scales, fmt, rows, dtype))       # the same bits each time
 
 
-@pytest.mark.parametrize("form", [11, 21, 22, 44, 88])
+@pytest.mark.parametrize("form", [11, 21, 22, 44, 84, 88])
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("rows,k,n,bias,act", [(1, 32, 1, False, 0), (5, 96, 40, True, 1), (129, 130, 145, True, 0), (255, 1025, 700, False, 1), (257, 544, 260, True, 0), (300, 4100, 64, False, 0)])
