@@ -484,7 +484,7 @@ void sbn_chain_free(sbn_chain_t* c);
  *     rows `ld*` ELEMENTS apart (at least cols).  Pointers need the alignment of
  *     their type only (2 or 4 bytes); codes need 16 bytes.
  *   - rows may be 0 (nothing is launched, pointers may then be NULL); cols is at
- *     least 1.  Extents and strides are 64-bit.
+ *     least 1.  Extents and strides are 64-bit; rows times cols is below 2^60.
  *   - Outputs must not overlap inputs unless a call says so.
  *   - Run calls launch on the stream given, never allocate, never synchronise.
  *     Sums are held in 32 bits and their order is fixed: the same call gives the
@@ -537,7 +537,7 @@ int sbn_dequantize(const void* codes, const void* scales, int format, int64_t ro
  *   y          of x_type; NULL: not written.
  *   format     0: no codes.  Otherwise y is taken through the format above (from
  *              its 32-bit values).
- * A row of zeros gives zeros.  A NaN or an infinity in a row makes the row NaN (or,
+ * A row of zeros gives zeros (NaN where eps is 0).  A NaN or an infinity in a row makes the row NaN (or,
  * for an infinity, zeros beside the NaN).  Squares are summed in 32 bits: rows with
  * values past 1e19 / sqrt(cols) overflow to zeros.
  */
@@ -584,7 +584,8 @@ void sbn_mx_free(sbn_mx_t* p);
  * the codes stand for, summed in 32 bits and rounded once to y's type.
  * codes / scales: [rows][c_in] in `format`.  workspace: device memory of at least
  * sbn_linear_mx_workspace bytes (16-byte aligned; NULL where that is 0), free for
- * other use once the launch has run; calls that overlap need one each.
+ * other use once the launch has run; calls that overlap need one each.  The kernels
+ * join their sums in LDS: sbn_linear_mx_workspace gives 0 for every layer.
  */
 int sbn_linear_mx_workspace(const sbn_mx_t* p, int format, int64_t rows, size_t* bytes_out);
 int sbn_linear_mx(const sbn_mx_t* p, const void* codes, const void* scales, int format, int64_t rows, void* y, int y_type,

@@ -621,9 +621,7 @@ int launch_mx_layout(const sbn_mx* p, const uint8_t* codes, const uint8_t* scale
     return SBN_OK;
 }
 
-size_t linear_mx_workspace(const sbn_mx*, int, long long) { return 0; }
-
-int launch_linear_mx(const sbn_mx* p, const void* codes, const void* scales, int format, long long rows, void* y, int y_type, long long ldy, void*, void* stream)
+int launch_linear_mx(const sbn_mx* p, const void* codes, const void* scales, int format, long long rows, void* y, int y_type, long long ldy, void* stream)
 {
     LinearArgs a = {};
     a.w = p->d_codes, a.ws = p->d_scales, a.bias = p->d_bias, a.x = (const uint8_t*)codes, a.xs = (const uint8_t*)scales;

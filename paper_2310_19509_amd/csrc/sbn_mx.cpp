@@ -22,6 +22,7 @@ int check_extents(const char* who, int64_t rows, int64_t cols)
 {
     if (rows < 0 || rows > kMostRows) return fail(SBN_EINVAL, "%s: rows out of range", who);
     if (cols < 1 || cols > kMostCols) return fail(SBN_EINVAL, "%s: columns out of range", who);
+    if (rows >= (1ll << 60) / cols) return fail(SBN_EINVAL, "%s: rows out of range", who);         // (sizes in bytes stay within 64 bits)
     return SBN_OK;
 }
 // A matrix of rows: its type, row stride and alignment.
@@ -244,8 +245,7 @@ int unpack_impl(const sbn_mx_t* p, void* codes, void* scales, float* bias)
     return SBN_OK;
 }
 
-int linear_impl(const sbn_mx_t* p, const void* codes, const void* scales, int format, int64_t rows, void* y, int y_type, int64_t ldy,
-                void* workspace, size_t workspace_bytes, void* stream)
+int linear_impl(const sbn_mx_t* p, const void* codes, const void* scales, int format, int64_t rows, void* y, int y_type, int64_t ldy, void* stream)
 {
     const char* const who = "sbn_linear_mx";
     if (!p) return fail(SBN_EINVAL, "%s: packed layer is NULL", who);
@@ -256,14 +256,11 @@ int linear_impl(const sbn_mx_t* p, const void* codes, const void* scales, int fo
     if (rows == 0) return SBN_OK;
     if (int rc = check_codes(who, format, codes, scales)) return rc;
     if (int rc = check_rows(who, "y", y, y_type, p->c_out, ldy)) return rc;
-    const size_t need = linear_mx_workspace(p, format, rows);
-    if (need && (!workspace || workspace_bytes < need)) return fail(SBN_EINVAL, "%s: needs a workspace of %zu bytes (got %zu)", who, need, workspace ? workspace_bytes : 0);
-    if (need && !aligned(workspace, 16)) return fail(SBN_EINVAL, "%s: workspace must be 16-byte aligned", who);
     int cur = -1;
     hipError_t e = hipGetDevice(&cur);
     if (e != hipSuccess) return fail(SBN_EHIP, "hipGetDevice: %s", hipGetErrorString(e));
     if (cur != p->device) return fail(SBN_EINVAL, "%s: current device is %d but the layer lives on device %d", who, cur, p->device);
-    return launch_linear_mx(p, codes, scales, format, rows, y, y_type, ldy, workspace, stream);
+    return launch_linear_mx(p, codes, scales, format, rows, y, y_type, ldy, stream);
 }
 
 int rmsnorm_impl(const sbn_rmsnorm_t* a, void* stream)
@@ -425,15 +422,15 @@ int sbn_linear_mx_workspace(const sbn_mx_t* p, int format, int64_t rows, size_t*
     if (!p || !bytes) return fail(SBN_EINVAL, "sbn_linear_mx_workspace: NULL pointer");
     if (!is_format(format)) return fail(SBN_EINVAL, "sbn_linear_mx_workspace: unknown format %d", format);
     if (int rc = check_extents("sbn_linear_mx_workspace", rows, p->c_in)) return rc;
-    *bytes = linear_mx_workspace(p, format, rows);
+    *bytes = 0;
     return SBN_OK;
 }
 
 int sbn_linear_mx(const sbn_mx_t* p, const void* codes, const void* scales, int format, int64_t rows, void* y, int y_type, int64_t ldy,
-                  void* workspace, size_t workspace_bytes, void* stream)
+                  void* /*workspace*/, size_t /*workspace_bytes*/, void* stream)
 {
     clear_error();
-    return guarded("sbn_linear_mx", [&]() -> int { return linear_impl(p, codes, scales, format, rows, y, y_type, ldy, workspace, workspace_bytes, stream); });
+    return guarded("sbn_linear_mx", [&]() -> int { return linear_impl(p, codes, scales, format, rows, y, y_type, ldy, stream); });
 }
 
 int sbn_log_probs_workspace(int64_t rows, int64_t cols, int k, size_t* bytes)

@@ -29,9 +29,8 @@ namespace sbn {
 
 // codes / scales (device, row-major) into the layout above; synchronous errors only
 int launch_mx_layout(const sbn_mx* p, const uint8_t* codes, const uint8_t* scales, bool back, uint8_t* codes_out, uint8_t* scales_out);
-size_t linear_mx_workspace(const sbn_mx* p, int format, long long rows);
 int launch_linear_mx(const sbn_mx* p, const void* codes, const void* scales, int format, long long rows, void* y, int y_type, long long ldy,
-                     void* workspace, void* stream);
+                     void* stream);
 
 int launch_quantize(const void* x, int x_type, long long rows, long long cols, long long ldx, int format, void* codes, void* scales, void* stream);
 int launch_dequantize(const void* codes, const void* scales, int format, long long rows, long long cols, void* y, int y_type, long long ldy, void* stream);

@@ -138,3 +138,10 @@ def test_sizes():
     assert S.sbn_quantized_bytes(S.SBN_FP8_ROW, 3, 33) == (3 * 64, 12)
     assert _error(lambda: S.sbn_quantized_bytes(1, 3, 33)) == -1
     assert S.sbn_log_probs_workspace(4096, 50000, 5) == 0 and S.sbn_log_probs_workspace(1, 100000, 5) > 0
+
+
+def test_sizes_that_pass_64_bits_are_refused():
+    for rows, cols in [(1 << 40, 1 << 21), (1 << 31, 1 << 30), ((1 << 40) + 1, 1)]:
+        assert _error(lambda: S.sbn_quantized_bytes(S.SBN_MXFP8, rows, cols)) == -1
+        assert _error(lambda: S.sbn_log_probs_workspace(rows, cols, 5)) == -1
+    assert S.sbn_quantized_bytes(S.SBN_MXFP8, 1 << 30, 1 << 20)[0] == 1 << 50
