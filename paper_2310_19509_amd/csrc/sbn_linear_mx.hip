@@ -268,14 +268,17 @@ __device__ inline void load_to_lds(u4 buffer, unsigned offset, unsigned scalar_o
 // 128 bytes (one step, twice as long) of 8-bit ones.  Rows go from memory straight to LDS, into the half of a double buffer that is not being read; weights go straight
 // to registers (a tile of the layout is one 16-byte load per lane), as only the WM waves side by side want the same ones.  One wait and one barrier
 // a stage, at its top.
-// Sixteen-byte pieces of a row lie at piece ^ (row & 7), which spreads the reads of eight rows over all banks.
+// Sixteen-byte pieces of a row lie at piece ^ (row & TURN), which spreads the reads of as many rows over all banks (4-bit rows at piece ^ (row & 7):
+// the same time, and LDS busy 25 % of it instead of 14 %).
+// Everything else that a wave does is spread between the multiplies, four (8-bit rows: two) at a time: the next row tile read from LDS, a tile of weights, two loads of rows.  In one lump for
+// every sixteen multiplies, as they come first to mind: 8192^3 in 4 bits 261 us instead of 249, 1024 x 4096 x 4096 15.2 instead of 14.3.
 // Scales of rows are turned, four steps at a time, into words that hold a lane's bytes of four steps, as the weights' are.
 // The last four steps are whole: past c_in they multiply zeros (leaving the loop among them would cost registers for every sum).
 template <int MODE, bool BLOCKS, class T, int MT, int NT, int WN, int WM>
 __global__ __launch_bounds__(64 * WN * WM, MT * NT > 32 ? 1 : 2) void tile_kernel(const LinearArgs a, const unsigned tiles_n, const unsigned tiles_m)
 {
     constexpr int THREADS = 64 * WN * WM, CH = 16 * MT * WN, RW = 16 * NT * WM, SB = MODE == kNarrow ? 256 : 128, SPS = MODE == kNarrow ? 4 : 1, SPQ = 4 / SPS;
-    constexpr int PIECES = SB / 16, NL = RW * PIECES / THREADS;            // pieces of a row's stage, loads of a wave for it
+    constexpr int PIECES = SB / 16, TURN = PIECES - 1, NL = RW * PIECES / THREADS;          // pieces of a row's stage, loads of a wave for it
     static_assert(RW <= THREADS && NL >= 1, "a row's scales belong to one thread");
     __shared__ __attribute__((aligned(16))) uint8_t lds_x[2][RW * SB];
     __shared__ unsigned lds_s[BLOCKS ? 2 : 1][BLOCKS ? THREADS * 4 : 1];  // (as many rows as threads: all of them write)
@@ -295,10 +298,10 @@ __global__ __launch_bounds__(64 * WN * WM, MT * NT > 32 ? 1 : 2) void tile_kerne
     const int rows = (int)min((long long)RW, a.rows - row0);
     const int stride = a.blocks * (MODE == kNarrow ? 16 : 32);            // bytes of a row's codes
 
-    // rows: a load of a wave is 64 / PIECES rows; lane l has piece (l % PIECES) ^ (row & 7) of row l / PIECES of them
+    // rows: a load of a wave is 64 / PIECES rows; lane l has piece (l % PIECES) ^ (row & TURN) of row l / PIECES of them
     const uint8_t* const x0 = a.x + row0 * stride;
     const u4 xr = {uniform((unsigned)(uintptr_t)x0), uniform((unsigned)((uintptr_t)x0 >> 32)), (unsigned)(rows * stride), 0x00020000u};
-    const int x_row = wave * (64 / PIECES) + lane / PIECES, x_piece = lane % PIECES ^ (x_row & 7);
+    const int x_row = wave * (64 / PIECES) + lane / PIECES, x_piece = lane % PIECES ^ (x_row & TURN);
     const unsigned x_off = (unsigned)(x_row * stride + x_piece * 16), lds_rows = uniform((unsigned)(uintptr_t)(__attribute__((address_space(3))) uint8_t*)&lds_x[0][0]) + wave * 1024;
     auto fetch_rows = [&](int stage, int from, int to) {
         // past the row's codes, and past the last row: past the buffer's end, where zeros are read
@@ -320,6 +323,7 @@ __global__ __launch_bounds__(64 * WN * WM, MT * NT > 32 ? 1 : 2) void tile_kerne
     };
     auto keep_scales = [&](int q) {
         if constexpr (BLOCKS) {
+            asm volatile("" : "+v"(sv));                                  // (or the compiler turns them, and waits for them, where they were asked for)
             const int left = a.blocks - q * 16;                           // blocks of the row in this quad and after
             const int over = max(t * a.blocks + q * 16 - most, 0);        // bytes that the load slid back
             const u4 d = over & 8 ? (u4){sv.z, sv.w, 0, 0} : sv;
@@ -345,10 +349,10 @@ __global__ __launch_bounds__(64 * WN * WM, MT * NT > 32 ? 1 : 2) void tile_kerne
     const long long base = min(first, a.tile_rows - 1);
     const auto buffer_at = [](const uint8_t* p) { return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p), 0, 0x7FFFFFFF, 0x00020000); };
     const __amdgpu_buffer_rsrc_t wr = buffer_at(a.w + base * a.steps * 1024), wsr = buffer_at(a.ws + base * a.quads * 256);
-    auto fetch_weights = [&](u4 (&to)[MT], int step) {
+    auto fetch_weights = [&](u4 (&to)[MT], int step, int from = 0, int end = MT) {
         const int at = min(step, a.steps - 1);
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int i = from; i < end; ++i)
             to[i] = __builtin_bit_cast(u4, __builtin_amdgcn_raw_buffer_load_b128(wr, lane * 16, (max(min(i, last), 0) * a.steps + at) * 1024, 0));
     };
     unsigned ws[MT];
@@ -367,7 +371,7 @@ __global__ __launch_bounds__(64 * WN * WM, MT * NT > 32 ? 1 : 2) void tile_kerne
 
     f4 acc[MT][NT] = {};
     const uint8_t* const x_lane = &lds_x[0][(wm * NT * 16 + r) * SB];
-    const int piece0 = (g ^ (r & 7)) * 16, piece1 = piece0 ^ 64;           // where pieces g and 4 + g of the lane's row lie
+    const int piece0 = (g ^ (r & TURN)) * 16;                               // where piece g of the lane's row lies
     // one step of 128 channels in bfloat16; u is its place in the stage, s in the quad
     auto multiply_wide = [&](const u4 (&w)[MT], const unsigned (&xs)[NT], int buffer, int u, int s) {
         const uint8_t* const x = x_lane + buffer * (RW * SB);
@@ -376,7 +380,7 @@ __global__ __launch_bounds__(64 * WN * WM, MT * NT > 32 ? 1 : 2) void tile_kerne
             b8 B[NT];
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                const u2 c = *(const u2*)(x + j * (16 * SB) + u * 128 + ((2 * g + k / 2) ^ (r & 7)) * 16 + k % 2 * 8);
+                const u2 c = *(const u2*)(x + j * (16 * SB) + u * 128 + ((2 * g + k / 2) ^ (r & TURN)) * 16 + k % 2 * 8);
                 B[j] = wide8(c.x, c.y, mx_scale(xs[j] >> 8 * s & 255u));
             }
 #pragma unroll
@@ -387,27 +391,22 @@ __global__ __launch_bounds__(64 * WN * WM, MT * NT > 32 ? 1 : 2) void tile_kerne
             }
         }
     };
-    // The scaled multiplies take a stage in chunks of NB row tiles, a chunk's rows read from LDS while the one before it is multiplied.
+    // The scaled multiplies take a stage in chunks of NB row tiles, a chunk's rows read from LDS while the one before it is multiplied, and a chunk by tiles of
+    // weights.
     constexpr int NB = MODE == kNarrow ? (NT < 4 ? NT : 4) : 2, CPS = NT / NB;          // chunks of a step
     i8v B[2][NB];
-    auto read_chunk = [&](int c, int buffer) {
+    auto read_tile = [&](int c, int j, int buffer) {
         const int u = c / CPS, j0 = c % CPS * NB;
-        const uint8_t* const x = x_lane + buffer * (RW * SB);
-        auto piece = [&](int j, int p) { return *(const u4*)(x + j * (16 * SB) + p / 8 * 128 + (p / 4 % 2 ? piece1 : piece0)); };          // (p without g)
-#pragma unroll
-        for (int j = 0; j < NB; ++j) {
-            const u4 lo = MODE == kNarrow ? piece(j0 + j, u * 4) : piece(j0 + j, u * 8), hi = MODE == kNarrow ? (u4){} : piece(j0 + j, u * 8 + 4);
-            B[c & 1][j] = (i8v){(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
-        }
+        const uint8_t* const x = x_lane + buffer * (RW * SB) + (j0 + j) * (16 * SB);
+        auto piece = [&](int p) { return *(const u4*)(x + (piece0 ^ p * 16)); };          // (p without g)
+        const u4 lo = MODE == kNarrow ? piece(u * 4) : piece(u * 8), hi = MODE == kNarrow ? (u4){} : piece(u * 8 + 4);
+        B[c & 1][j] = (i8v){(int)lo.x, (int)lo.y, (int)lo.z, (int)lo.w, (int)hi.x, (int)hi.y, (int)hi.z, (int)hi.w};
     };
-    auto multiply_chunk = [&](int c, const u4 (&w)[MT], const unsigned (&xs)[NT], int s) {
+    auto multiply_tile = [&](int c, int i, const u4 (&w)[MT], const unsigned (&xs)[NT], int s) {
         const int j0 = c % CPS * NB;
+        const i8v A = {(int)w[i].x, (int)w[i].y, (int)w[i].z, (int)w[i].w, 0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const i8v A = {(int)w[i].x, (int)w[i].y, (int)w[i].z, (int)w[i].w, 0, 0, 0, 0};
-#pragma unroll
-            for (int j = 0; j < NB; ++j) acc[i][j0 + j] = scaled_mma<MODE == kNarrow ? 4 : 0>(A, B[c & 1][j], acc[i][j0 + j], s, ws[i], xs[j0 + j]);
-        }
+        for (int j = 0; j < NB; ++j) acc[i][j0 + j] = scaled_mma<MODE == kNarrow ? 4 : 0>(A, B[c & 1][j], acc[i][j0 + j], s, ws[i], xs[j0 + j]);
     };
 
     // Weights are asked for two steps ahead (8-bit rows: one, their steps are twice as long); the rows of the next stage during this one's first step.
@@ -425,7 +424,9 @@ __global__ __launch_bounds__(64 * WN * WM, MT * NT > 32 ? 1 : 2) void tile_kerne
         for (int st = 0; st < SPQ; ++st) {
             const int stage = q * SPQ + st, buffer = stage & 1;
             landed();
-            if constexpr (MODE != kWide8) read_chunk(0, buffer);
+            if constexpr (MODE != kWide8)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) read_tile(0, j, buffer);
             if (st == 0) {
 #pragma unroll
                 for (int j = 0; j < NT; ++j) xs[j] = BLOCKS ? lds_s[q & 1][(wm * NT + j) * 64 + lane] : 127u * 0x01010101u;
@@ -435,8 +436,8 @@ __global__ __launch_bounds__(64 * WN * WM, MT * NT > 32 ? 1 : 2) void tile_kerne
 #pragma unroll
             for (int u = 0; u < SPS; ++u) {
                 const int s = st * SPS + u;
-                fetch_weights(w[(s + AHEAD) % SETS], q * 4 + s + AHEAD);
                 if constexpr (MODE == kWide8) {
+                    fetch_weights(w[(s + AHEAD) % SETS], q * 4 + s + AHEAD);
                     if (u == 0) fetch_rows(stage + 1, 0, NL);             // (past the last stage: zeros, into the half that nothing reads any more)
                     __builtin_amdgcn_sched_barrier(0);
                     if (s == 3) keep_scales(q + 1);
@@ -444,14 +445,21 @@ __global__ __launch_bounds__(64 * WN * WM, MT * NT > 32 ? 1 : 2) void tile_kerne
                     __builtin_amdgcn_sched_barrier(0);
                 } else {
 #pragma unroll
-                    for (int c = 0; c < CPS; ++c) {
-                        if (u * CPS + c + 1 < SPS * CPS) read_chunk(u * CPS + c + 1, buffer);
-                        if (u == 0) fetch_rows(stage + 1, NL * c / CPS, NL * (c + 1) / CPS);
-                        __builtin_amdgcn_sched_barrier(0);
-                        multiply_chunk(u * CPS + c, w[s % SETS], xs, s);
-                        if (s == 3 && c == 0) keep_scales(q + 1);
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
+                    for (int c = 0; c < CPS; ++c)
+#pragma unroll
+                        for (int i = 0; i < MT; ++i) {
+                            constexpr int PARTS = CPS * MT;
+                            const int part = c * MT + i, next = u * CPS + c + 1;
+                            __builtin_amdgcn_sched_barrier(0);            // (first what is to come: with the multiplies first the sums change registers)
+                            if (next < SPS * CPS)
+#pragma unroll
+                                for (int j = NB * i / MT; j < NB * (i + 1) / MT; ++j) read_tile(next, j, buffer);
+                            if (c == 0) fetch_weights(w[(s + AHEAD) % SETS], q * 4 + s + AHEAD, i, i + 1);
+                            if (u == 0) fetch_rows(stage + 1, NL * part / PARTS, NL * (part + 1) / PARTS);
+                            if (s == 3 && part == PARTS - 1) keep_scales(q + 1);
+                            __builtin_amdgcn_sched_barrier(0);
+                            multiply_tile(u * CPS + c, i, w[s % SETS], xs, s);
+                        }
                 }
             }
         }
@@ -472,6 +480,12 @@ __global__ __launch_bounds__(64 * WN * WM, MT * NT > 32 ? 1 : 2) void tile_kerne
     if constexpr (FMT == SBN_FP8_ROW)
 #pragma unroll
         for (int j = 0; j < NT; ++j) row_scale[j] = ((const float*)a.xs)[row0 + min((wm * NT + j) * 16 + r, rows - 1)];
+    // all here before the first store: a later wait for them would wait for the stores too, at every edge that branches
+#pragma unroll
+    for (int i = 0; i < MT; ++i) asm volatile("" : "+v"(bias[i]));
+    if constexpr (FMT == SBN_FP8_ROW)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) asm volatile("" : "+v"(row_scale[j]));
     const bool relu = a.act == SBN_ACT_RELU, whole = rows == RW && (int)(tile_n + 1) * CH <= a.c_out;
     auto finished = [&](int i, int j) {
         f4 v = acc[i][j];
@@ -536,9 +550,9 @@ void launch_few(const LinearArgs& a, hipStream_t stream)
 //   tiles: 3, and so much plus so much per 128 input channels for every two tiles a compute unit, which it has at work at a time, and
 //     for a last one that it works on alone.  (256 rows x 256 channels leave no room for two.)  On three shapes, in 4 bits:
 //                                128 x 128   128 rows x 256   256 x 256
-//        1024 x 4096 x  4096       16 us          19              30
-//        2048 x 4096 x 11000       65             53              67
-//        8192 x 8192 x  8192      339            260             248
+//        1024 x 4096 x  4096       14 us          17              29
+//        2048 x 4096 x 11000       68             54              65
+//        8192 x 8192 x  8192      343            263             249
 //     Rows in 8 bits: 256 x 256 are never the best, 8192^3 in 473, 377 and 387.  32-bit results of them: 128 x 128 alone, as the
 //     conversions to bfloat16 leave no registers for more (128 x 256: 142 us of 4096^3, 114).
 struct TileCost {
