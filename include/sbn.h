@@ -487,7 +487,7 @@ void sbn_chain_free(sbn_chain_t* c);
  *     least 1.  Extents and strides are 64-bit; rows times cols is below 2^60.
  *   - Outputs must not overlap inputs unless a call says so.
  *   - Run calls launch on the stream given, never allocate, never synchronise.
- *     Sums are held in 32 bits and their order is fixed: the same call gives the
+ *     Sums are held in 32 bits or more and their order is fixed: the same call gives the
  *     same bits.
  */
 #define SBN_F32  0
@@ -535,11 +535,12 @@ int sbn_dequantize(const void* codes, const void* scales, int format, int64_t ro
  *              the types and ld agree.
  *   weight     float [cols]; NULL: ones.
  *   y          of x_type; NULL: not written.
- *   format     0: no codes.  Otherwise y is taken through the format above (from
- *              its 32-bit values).
+ *   format     0: no codes.  Otherwise y is taken through the format above.
+ * The squares are summed in 64 bits, and y and the codes are rounded once each, from
+ * 64-bit values.
  * A row of zeros gives zeros (NaN where eps is 0).  A NaN or an infinity in a row makes the row NaN (or,
- * for an infinity, zeros beside the NaN).  Squares are summed in 32 bits: rows with
- * values past 1e19 / sqrt(cols) overflow to zeros.
+ * for an infinity, zeros beside the NaN).  A row whose squares sum to more than
+ * 32 bits hold (values past 1e19 / sqrt(cols)) gives zeros.
  */
 typedef struct {
     int64_t rows, cols;

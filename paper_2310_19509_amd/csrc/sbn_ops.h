@@ -188,10 +188,10 @@ __device__ inline u2 codes8(const float (&v)[8], float scale)
     return r;
 }
 
-// f over a wave's values, the same bits on all lanes; f(a, b) and f(b, a) have to have the same.  Lanes of a row of 16 are paired by moves within the
+// f over the values of N neighbouring lanes (all of a wave), the same bits on all of them; f(a, b) and f(b, a) have to have the same.  Lanes of a row of 16 are paired by moves within the
 // vector unit (1 0 3 2, 2 3 0 1, then rows of 8 and of 16 mirrored, whose halves agree by then), rows by swaps: no step waits for LDS.
 // Against exchanges through LDS: norm of one row of 8192 4.0 -> 3.6 us, scores of 64 rows of 32768, twenty alternatives, 13.0 -> 12.0.
-template <class V, class F>
+template <int N = 64, class V, class F>
 __device__ inline V wave_all(V v, F f)
 {
     struct Words {
@@ -205,8 +205,8 @@ __device__ inline V wave_all(V v, F f)
     };
     move(std::integral_constant<int, 0xB1>{});
     move(std::integral_constant<int, 0x4E>{});
-    move(std::integral_constant<int, 0x141>{});
-    move(std::integral_constant<int, 0x140>{});
+    if constexpr (N > 4) move(std::integral_constant<int, 0x141>{});
+    if constexpr (N > 8) move(std::integral_constant<int, 0x140>{});
     const auto swap = [&](auto wide) {
         Words a = __builtin_bit_cast(Words, v), b = a;
 #pragma unroll
@@ -216,18 +216,19 @@ __device__ inline V wave_all(V v, F f)
         }
         v = f(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b));
     };
-    swap(std::false_type{});
-    swap(std::true_type{});
+    if constexpr (N > 16) swap(std::false_type{});
+    if constexpr (N > 32) swap(std::true_type{});
     return v;
 }
-__device__ inline float wave_sum(float v)
+template <int N = 64, class V>
+__device__ inline V wave_sum(V v)
 {
-    return wave_all(v, [](float a, float b) { return a + b; });
+    return wave_all<N>(v, [](V a, V b) { return a + b; });
 }
-template <class V>
+template <int N = 64, class V>
 __device__ inline V wave_max(V v)
 {
-    return wave_all(v, [](V a, V b) { return a > b ? a : b; });
+    return wave_all<N>(v, [](V a, V b) { return a > b ? a : b; });
 }
 // The largest of four neighbouring lanes: the 32 columns of a block.
 __device__ inline unsigned quad_max(unsigned v)

@@ -28,7 +28,8 @@ __device__ inline void put_block_codes(const float (&v)[8], void* codes, uint8_t
     if ((at & 3) == 0) scales[at >> 2] = (uint8_t)byte;
 }
 
-// Blocks.  A thread takes kItems units of the launch's rows, a workgroup apart.
+// Blocks.  A thread takes kItems units of the launch's rows, a workgroup apart.  8192 x 8192 in bfloat16: to 4 bits 30 us, 5.7 TB/s read and written, and back
+// (dequantize_kernel) 26, 6.4 TB/s; one row 1.9 us, what a launch takes.
 constexpr int kItems = 4;
 template <class T, int FMT, bool ONCE>
 __global__ __launch_bounds__(256) void quantize_kernel(const T* __restrict__ x, long long ldx, unsigned units, unsigned total,
@@ -99,7 +100,7 @@ __global__ __launch_bounds__(256) void dequantize_kernel(const void* __restrict_
     }
 }
 
-// What the row kernel needs.  `norm` 0: y = x (the row format of plain rows).
+// What the row kernels need.
 struct RowArgs {
     long long rows, cols, ldx, ldr, ldt, ldy;
     const void* x;
@@ -110,76 +111,70 @@ struct RowArgs {
     void* codes;
     void* scales;
     float eps;
-    int norm, format;
+    int format;
+    double share;                          // 1 / cols
 };
+struct PlainRows {};                       // as a residual's type: rows into SBN_FP8_ROW without a norm
 
-struct Root {                              // 1 / sqrt(mean + eps) as a sum of two floats
-    float hi, lo;
-};
-__device__ inline Root inverse_root(float sum, long long cols, float eps)
+// The norm is in 64 bits from the sum of the squares on, so that codes go where the exact value goes.  In 32 bits, with one rounding of h w / rms and one of each
+// step to a row's codes, 26 to 43 of 2^26 codes lay on the other side of a tie (38 to 57 with 32-bit operations one by one); now none does.  16384 x 4096
+// in 16 bits takes 83.4 us for 81.4, 1021 x 5001 12.8 for 11.6.
+__device__ inline double inverse_root(double sum, double share, float eps)
 {
-    const float s = sum / (float)cols + eps;
-    Root r;
-    r.hi = rsqrtf(s);
-    // one Newton step kept apart: the residue 1 - s r^2 with the product's own rounding in it
-    const float t = s * r.hi, te = __builtin_fmaf(s, r.hi, -t);
-    const float e = __builtin_fmaf(-t, r.hi, 1.0f) - te * r.hi;
-    r.lo = s > 0.0f && s < __builtin_inff() ? 0.5f * r.hi * e : 0.0f;
+    const double s = __builtin_fma(sum, share, (double)eps);
+    if (sum > 3.4028234663852886e38 || s > 3.4028234663852886e38) return 0.0;                 // (past 32 bits: as infinity)
+    double r = __builtin_amdgcn_rsq(s);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) r = __builtin_fma(__builtin_fma(-0.5 * s * r, r, 0.5), r, r); // Newton: r + r (1 - s r^2) / 2, from 20 bits or more
     return r;
 }
-// h * w / rms with one rounding: codes that lie near a tie go where the exact value goes, up to the sum's own error.
-__device__ inline float normed(float h, float w, const Root& r)
+// x to 32 bits, cut, the last bit set where something was cut off: a rounding to fewer bits then rounds x itself.
+__device__ inline float odd32(double x)
 {
-    const float p = h * w, e = __builtin_fmaf(h, w, -p);
-    return __builtin_fmaf(p, r.hi, __builtin_fmaf(p, r.lo, e * r.hi));
+    const unsigned long long b = __builtin_bit_cast(unsigned long long, x);
+    const unsigned lo = (unsigned)b, cut = lo & 0x1FFFFFFFu, sticky = (cut + 0x1FFFFFFFu) & 0x20000000u;
+    return (float)__builtin_bit_cast(double, (b >> 32 << 32) | (lo & 0xE0000000u) | sticky);
 }
 
 // Sum / largest over a row's threads, the same on all of them.
 template <int THREADS>
-__device__ inline float row_sum(float v, float* lds)
+__device__ inline double row_sum(double v, double* lds)
 {
+    constexpr int WAVES = THREADS / 64;
     v = wave_sum(v);
-    if constexpr (THREADS > 64) {
+    if constexpr (WAVES > 1) {
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
         __syncthreads();
-        v = 0.0f;
-#pragma unroll
-        for (int i = 0; i < THREADS / 64; ++i) v += lds[i];
+        v = wave_sum<WAVES>(lds[threadIdx.x % WAVES]);
     }
     return v;
 }
-template <int THREADS>
-__device__ inline unsigned row_max(unsigned v, unsigned* lds)
+template <int THREADS, class V>
+__device__ inline V row_max(V v, V* lds)
 {
+    constexpr int WAVES = THREADS / 64;
     v = wave_max(v);
-    if constexpr (THREADS > 64) {
+    if constexpr (WAVES > 1) {
         if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
         __syncthreads();
-        v = 0;
-#pragma unroll
-        for (int i = 0; i < THREADS / 64; ++i) v = max(v, lds[i]);
+        v = wave_max<WAVES>(lds[threadIdx.x % WAVES]);
     }
     return v;
 }
 
-template <class XT>
-__device__ inline void put_row_outputs(const RowArgs& a, long long row, long long unit, const float (&v)[8], float inverse)
+typedef unsigned long long Bits64;
+// The bits of the largest magnitude, ordered as those of 32 bits are.
+__device__ inline Bits64 top_bits64(const double (&p)[8])
 {
-    const long long at = row * units_of(a.cols) + unit;
-    if (a.y && unit * 8 < a.cols) store_unit((XT*)a.y + row * a.ldy, unit, a.cols, v);
-    if (a.format == SBN_MXFP4) {
-        put_block_codes<SBN_MXFP4>(v, a.codes, (uint8_t*)a.scales, at);
-    } else if (a.format == SBN_MXFP8) {
-        put_block_codes<SBN_MXFP8>(v, a.codes, (uint8_t*)a.scales, at);
-    } else if (a.format == SBN_FP8_ROW) {
-        float q[8];
+    Bits64 t = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) q[j] = v[j] * inverse;
-        ((u2*)a.codes)[at] = codes8(q, 1.0f);
+    for (int j = 0; j < 8; ++j) {
+        const Bits64 b = __builtin_bit_cast(Bits64, p[j]) & ~(1ull << 63);
+        t = b > t ? b : t;
     }
+    return t;
 }
-
-// scale and 448 (1 / a) of a row from the bits of its largest magnitude
+// A row's scale and the factor of its codes.  Plain: scale = a / 448, codes of x (448 (1 / a)), in steps of 32 bits; after a norm: codes of p factor, p = h w.
 __device__ inline float row_scale(unsigned top, float& inverse)
 {
     const float t = __builtin_bit_cast(float, top);
@@ -189,14 +184,49 @@ __device__ inline float row_scale(unsigned top, float& inverse)
     inverse = kTop8 * (1.0f / t);
     return t / kTop8;
 }
+__device__ inline float row_scale(Bits64 top, double root, double& factor)
+{
+    const double p = __builtin_bit_cast(double, top), t = p * root;
+    factor = 0.0;
+    if (!(t <= 3.4028234663852886e38)) return __builtin_nanf("");
+    if (t < (double)kLeastRow) return 0.0f;
+    double r = __builtin_amdgcn_rcp(p);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) r = __builtin_fma(__builtin_fma(-p, r, 1.0), r, r);
+    factor = (double)kTop8 * r;
+    return (float)(t * (1.0 / (double)kTop8));
+}
 
-// One row to THREADS threads, held in registers: ITEMS units each.  RT: the residual's type, or void.
+// A unit's outputs after a norm: y = p root; 16-bit y and codes are rounded once.
+template <class XT>
+__device__ inline void put_row_outputs(const RowArgs& a, long long row, long long unit, const double (&p)[8], double root, double factor)
+{
+    const long long at = row * units_of(a.cols) + unit;
+    float v[8];
+    if (a.y && unit * 8 < a.cols) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = sizeof(XT) == 2 ? odd32(p[j] * root) : (float)(p[j] * root);
+        store_unit((XT*)a.y + row * a.ldy, unit, a.cols, v);
+    }
+    const double by = a.format == SBN_FP8_ROW ? factor : root;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = odd32(p[j] * by);
+    if (a.format == SBN_MXFP4)
+        put_block_codes<SBN_MXFP4>(v, a.codes, (uint8_t*)a.scales, at);
+    else if (a.format == SBN_MXFP8)
+        put_block_codes<SBN_MXFP8>(v, a.codes, (uint8_t*)a.scales, at);
+    else if (a.format == SBN_FP8_ROW)
+        ((u2*)a.codes)[at] = codes8(v, 1.0f);
+}
+
+// One row to THREADS threads, held in registers: ITEMS units each.  RT: the residual's type, void for none, or PlainRows.  16384 x 4096, x and residual in
+// bfloat16, to rows of FP8: 470 MB in 83 us, 5.6 TB/s; one row of 8192 4.1 us.
 template <class XT, class RT, int THREADS, int ITEMS, bool ONCE = false>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void row_kernel(const RowArgs a)
 {
-    __shared__ float lds_sum[16];
-    __shared__ unsigned lds_max[16];
-    constexpr bool ADD = !std::is_same<RT, void>::value;
+    __shared__ double lds_sum[16];
+    __shared__ Bits64 lds_max[16];
+    constexpr bool NORM = !std::is_same<RT, PlainRows>::value, ADD = NORM && !std::is_same<RT, void>::value;
     using R = typename std::conditional<ADD, RT, XT>::type;
     const int t = threadIdx.x % THREADS;
     const long long row = THREADS < 256 ? (long long)blockIdx.x * (256 / THREADS) + threadIdx.x / THREADS : (long long)blockIdx.x;
@@ -214,11 +244,11 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void row_kernel(cons
         if constexpr (ADD) rr[i] = fetch_unit<ONCE>(res, i * THREADS + t, cols);
     }
     // Few rows wait for memory: their weights are asked for together with the rows.
-    constexpr bool EARLY = ITEMS == 1;
+    constexpr bool EARLY = NORM && ITEMS == 1;
     Raw<float> rw = {};
     if (EARLY && a.weight) rw = fetch_unit(a.weight, t, cols);
     float v[ITEMS][8];
-    float sum = 0.0f;
+    double sum = 0.0;
 #pragma unroll
     for (int i = 0; i < ITEMS; ++i) {
         const int unit = i * THREADS + t;
@@ -230,48 +260,63 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void row_kernel(cons
             for (int j = 0; j < 8; ++j) v[i][j] += b[j];
             if (a.total && (long long)unit * 8 < cols) store_unit((R*)a.total + row * a.ldt, unit, cols, v[i]);
         }
+        if constexpr (NORM)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum = __builtin_fmaf(v[i][j], v[i][j], sum);
+            for (int j = 0; j < 8; ++j) sum = __builtin_fma((double)v[i][j], (double)v[i][j], sum);
     }
-    if (a.norm) {
-        const Root root = inverse_root(row_sum<THREADS>(sum, lds_sum), cols, a.eps);
+    if constexpr (NORM) {
+        const double root = inverse_root(row_sum<THREADS>(sum, lds_sum), a.share, a.eps);
+        double p[ITEMS][8];
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
             const int unit = i * THREADS + t;
-            float w[8];
-            if (a.weight) {
-                expand_unit(EARLY ? rw : fetch_unit(a.weight, unit, cols), a.weight, unit, cols, w, 0.0f);
-            } else {
+            float w[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
+            if (a.weight) expand_unit(EARLY ? rw : fetch_unit(a.weight, unit, cols), a.weight, unit, cols, w, 0.0f);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) w[j] = 1.0f;
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] = normed(v[i][j], w[j], root);
+            for (int j = 0; j < 8; ++j) p[i][j] = (double)v[i][j] * (double)w[j];
         }
-    }
-    float inverse = 0.0f;
-    if (a.format == SBN_FP8_ROW) {
+        double factor = 0.0;
+        if (a.format == SBN_FP8_ROW) {
+            Bits64 top = 0;
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                const Bits64 b = top_bits64(p[i]);
+                top = b > top ? b : top;
+            }
+            const float scale = row_scale(row_max<THREADS>(top, lds_max), root, factor);
+            if (t == 0) ((float*)a.scales)[row] = scale;
+        }
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int unit = i * THREADS + t;
+            if (unit < units) put_row_outputs<XT>(a, row, unit, p[i], root, factor);
+        }
+    } else {
         unsigned top = 0;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) top = max(top, top_bits(v[i]));
-        const float scale = row_scale(row_max<THREADS>(top, lds_max), inverse);
+        float inverse;
+        const float scale = row_scale(row_max<THREADS>(top, (unsigned*)lds_max), inverse);
         if (t == 0) ((float*)a.scales)[row] = scale;
-    }
 #pragma unroll
-    for (int i = 0; i < ITEMS; ++i) {
-        const int unit = i * THREADS + t;
-        if (unit < units) put_row_outputs<XT>(a, row, unit, v[i], inverse);
+        for (int i = 0; i < ITEMS; ++i) {
+            const int unit = i * THREADS + t;
+            float q[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) q[j] = v[i][j] * inverse;
+            if (unit < units) ((u2*)a.codes)[row * units + unit] = codes8(q, 1.0f);
+        }
     }
 }
 
-// Rows that no workgroup's registers hold: read again for every step.  The sums x + residual are written in the last step
+// Rows that no workgroup's registers hold, from 32769 columns on: read again for every step, from L2 where they are not too many.  The sums x + residual are written in the last step
 // only, each by the lane that reads the same places, so that they may take their inputs' place.
 template <class XT, class RT>
 __global__ __launch_bounds__(1024) void long_row_kernel(const RowArgs a)
 {
-    __shared__ float lds_sum[16];
-    __shared__ unsigned lds_max[16];
-    constexpr bool ADD = !std::is_same<RT, void>::value;
+    __shared__ double lds_sum[16];
+    __shared__ Bits64 lds_max[16];
+    constexpr bool NORM = !std::is_same<RT, PlainRows>::value, ADD = NORM && !std::is_same<RT, void>::value;
     using R = typename std::conditional<ADD, RT, XT>::type;
     const long long row = blockIdx.x, cols = a.cols, units = units_of(cols);
     const XT* const x = (const XT*)a.x + row * a.ldx;
@@ -285,44 +330,61 @@ __global__ __launch_bounds__(1024) void long_row_kernel(const RowArgs a)
             for (int j = 0; j < 8; ++j) v[j] += b[j];
         }
     };
-    Root root = {1.0f, 0.0f};
-    if (a.norm) {
-        float sum = 0.0f;
+    if constexpr (NORM) {
+        double sum = 0.0;
         for (long long u = threadIdx.x; u < units; u += 1024) {
-            float v[8], part = 0.0f;
+            float v[8];
             get(u, v);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) part = __builtin_fmaf(v[j], v[j], part);
-            sum += part;
+            for (int j = 0; j < 8; ++j) sum = __builtin_fma((double)v[j], (double)v[j], sum);
         }
-        root = inverse_root(row_sum<1024>(sum, lds_sum), cols, a.eps);
-    }
-    auto finish = [&](long long unit, float (&v)[8]) {
-        if (!a.norm) return;
-        float w[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
-        if (a.weight) expand_unit(fetch_unit(a.weight, unit, cols), a.weight, unit, cols, w, 0.0f);
+        const double root = inverse_root(row_sum<1024>(sum, lds_sum), a.share, a.eps);
+        auto weighted = [&](long long unit, const float (&v)[8], double (&p)[8]) {
+            float w[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
+            if (a.weight) expand_unit(fetch_unit(a.weight, unit, cols), a.weight, unit, cols, w, 0.0f);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = normed(v[j], w[j], root);
-    };
-    float inverse = 0.0f;
-    if (a.format == SBN_FP8_ROW) {
+            for (int j = 0; j < 8; ++j) p[j] = (double)v[j] * (double)w[j];
+        };
+        double factor = 0.0;
+        if (a.format == SBN_FP8_ROW) {
+            Bits64 top = 0;
+            for (long long u = threadIdx.x; u < units; u += 1024) {
+                float v[8];
+                double p[8];
+                get(u, v);
+                weighted(u, v, p);
+                const Bits64 b = top_bits64(p);
+                top = b > top ? b : top;
+            }
+            const float scale = row_scale(row_max<1024>(top, lds_max), root, factor);
+            if (threadIdx.x == 0) ((float*)a.scales)[row] = scale;
+        }
+        for (long long u = threadIdx.x; u < units; u += 1024) {
+            float v[8];
+            double p[8];
+            get(u, v);
+            if constexpr (ADD)
+                if (a.total && u * 8 < cols) store_unit((R*)a.total + row * a.ldt, u, cols, v);
+            weighted(u, v, p);
+            put_row_outputs<XT>(a, row, u, p, root, factor);
+        }
+    } else {
         unsigned top = 0;
         for (long long u = threadIdx.x; u < units; u += 1024) {
             float v[8];
             get(u, v);
-            finish(u, v);
             top = max(top, top_bits(v));
         }
-        const float scale = row_scale(row_max<1024>(top, lds_max), inverse);
+        float inverse;
+        const float scale = row_scale(row_max<1024>(top, (unsigned*)lds_max), inverse);
         if (threadIdx.x == 0) ((float*)a.scales)[row] = scale;
-    }
-    for (long long u = threadIdx.x; u < units; u += 1024) {
-        float v[8];
-        get(u, v);
-        if constexpr (ADD)
-            if (a.total && u * 8 < cols) store_unit((R*)a.total + row * a.ldt, u, cols, v);
-        finish(u, v);
-        put_row_outputs<XT>(a, row, u, v, inverse);
+        for (long long u = threadIdx.x; u < units; u += 1024) {
+            float v[8];
+            get(u, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= inverse;
+            ((u2*)a.codes)[row * units + u] = codes8(v, 1.0f);
+        }
     }
 }
 
@@ -337,7 +399,7 @@ int launch_rows(RowArgs a, hipStream_t stream)
         const int fmt = a.format;
         const long long per = units * (fmt == SBN_MXFP4 ? 4 : 8);
         b.x = (const XT*)a.x + r0 * a.ldx;
-        if constexpr (!std::is_same<RT, void>::value) {
+        if constexpr (!std::is_same<RT, void>::value && !std::is_same<RT, PlainRows>::value) {
             b.residual = (const RT*)a.residual + r0 * a.ldr;
             if (a.total) b.total = (RT*)a.total + r0 * a.ldt;
         }
@@ -415,10 +477,11 @@ int launch_add_rmsnorm(const sbn_rmsnorm_t& n, bool norm, void* stream)
     RowArgs a = {};
     a.rows = n.rows, a.cols = n.cols, a.ldx = n.ldx, a.ldr = n.ldr, a.ldt = n.ldt, a.ldy = n.ldy;
     a.x = n.x, a.residual = n.residual, a.total = n.total, a.weight = n.weight, a.y = n.y, a.codes = n.codes, a.scales = n.scales;
-    a.eps = n.eps, a.norm = norm, a.format = n.format;
+    a.eps = n.eps, a.format = n.format, a.share = 1.0 / (double)n.cols;
     const hipStream_t s = (hipStream_t)stream;
     auto typed = [&](auto* t) -> int {
         using T = typename std::remove_pointer<decltype(t)>::type;
+        if (!norm) return launch_rows<T, PlainRows>(a, s);
         if (!n.residual) return launch_rows<T, void>(a, s);
         if (n.r_type == n.x_type) return launch_rows<T, T>(a, s);
         return launch_rows<T, float>(a, s);

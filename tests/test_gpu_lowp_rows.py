@@ -189,6 +189,25 @@ def test_norm_of_zero_nan_infinite_and_huge_rows():
     assert (y[0] == 0).all() and scales[0] == 0 and (codes[0] == 0).all()
 
 
+@pytest.mark.parametrize("rows,cols,xt,rt", [(2048, 4096, torch.bfloat16, torch.bfloat16), (1500, 1600, torch.float32, None), (700, 5001, torch.float16, torch.float32),
+                                             (3, 8192, torch.float32, torch.float32), (40, 40000, torch.bfloat16, None)])
+def test_norm_rounds_codes_once(rows, cols, xt, rt):
+    """Codes are those of the 64-bit values of the 32-bit sums x + residual: all of them, also next to a tie."""
+    x, w = _x(rows + cols, rows, cols, xt, 0, 1), torch.randn(cols, device="cuda")
+    r = None if rt is None else _x(rows * 3 + cols, rows, cols, rt, 0, 1)
+    y = L.rmsnorm(_np(x.float() if r is None else x.float() + r.float()), _np(w), float(np.float32(1e-6)))
+    for fmt in FORMATS:
+        codes, scales = S.sbn_quantized_empty(fmt, rows, cols)
+        S.sbn_add_rmsnorm(x, w, 1e-6, residual=r, fmt=fmt, codes=codes, scales=scales)
+        if fmt == S.SBN_FP8_ROW:
+            top = np.abs(y).max(1)
+            want, want_s = np.zeros(tuple(codes.shape), dtype=np.uint8), (top / 448).astype(np.float32)
+            want[:, :cols] = L.element_codes(y * (448 / np.where(top > 0, top, 1))[:, None], L.E4M3, 128)
+        else:
+            want, want_s = L.quantize(y, fmt)
+        assert np.array_equal(codes.cpu().numpy(), want) and np.array_equal(scales.cpu().numpy(), want_s)
+
+
 def test_rows_far_apart():
     """Offsets past 32 bits: rows 3 * 2^30 bytes apart."""
     ld = 3 << 29
