@@ -289,7 +289,7 @@ __global__ __launch_bounds__(64 * kWaves, TOP ? 4 : 1) void score_kernel(const T
     __shared__ unsigned tops[TOP && !SOLO ? kWaves : 1][64];
     __shared__ Stat stats[kWaves];
     __shared__ int counts[kWaves];
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const long long row = SOLO ? (long long)blockIdx.x * kWaves + wave : blockIdx.x / (unsigned)a.slices;
     if (SOLO && row >= a.rows) return;
     const unsigned slice = SOLO ? 0 : blockIdx.x % (unsigned)a.slices;
@@ -304,17 +304,43 @@ __global__ __launch_bounds__(64 * kWaves, TOP ? 4 : 1) void score_kernel(const T
     Search find;
     if constexpr (TOP) find.start(lists[wave], a.k, end);
     unsigned turn = 0, next_bound = 0;
-    // (the first turn has a barrier: all waves make it)
-    for (unsigned c0 = begin + (SOLO ? 0 : wave * kStep); c0 < end || (TOP && !SOLO && turn == 0); c0 += U * kTurn, ++turn) {
-        Raw<T> raw[U];
+    unsigned c0 = begin + (SOLO ? 0 : wave * kStep);
+    if constexpr (SOLO && !TOP && sizeof(T) == 2) {
+        // Long rows: eight steps under way, 2048 x 128000 94.6 -> 85.7 us, 8192 x 32768 97.4 -> 93.0.  Short ones spend as much on what is left over
+        // (16384 x 5000 36.6 -> 37.6), and 32-bit logits have as many bytes under way with four (2048 x 50001 72.2, 76.2 with eight).
+        constexpr int LONG = 8;
+        for (const unsigned stop = a.cols >= 16384 ? end : 0; c0 + LONG * kStep <= stop; c0 += LONG * kStep) {
+            Raw<T> raw[LONG];
 #pragma unroll
-        for (int u = 0; u < U; ++u) raw[u] = fetch_unit<ONCE>(x, (c0 + u * kTurn) / 8 + lane, end);
-        float v[U][8], top[U];
+            for (int u = 0; u < LONG; ++u) raw[u] = fetch<ONCE>(x + c0 + u * kStep + lane * 8);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            expand_unit(raw[u], x, (c0 + u * kTurn) / 8 + lane, end, v[u], -__builtin_inff());
-            top[u] = add(st, v[u]);
+            for (int u = 0; u < LONG; ++u) {
+                float v[8];
+                expand(raw[u], v);
+                add(st, v);
+            }
         }
+    }
+    // (the first turn has a barrier: all waves make it)
+    for (; c0 < end || (TOP && !SOLO && turn == 0); c0 += U * kTurn, ++turn) {
+        // Whole turns, all but a row's last, test no lane's columns.
+        const bool whole = c0 + (U - 1) * kTurn + kStep <= end;
+        Raw<T> raw[U];
+        float v[U][8], top[U];
+        if (whole) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) raw[u] = fetch<ONCE>(x + c0 + u * kTurn + lane * 8);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) raw[u] = fetch_unit<ONCE>(x, (c0 + u * kTurn) / 8 + lane, end);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) expand(raw[u], v[u]);
+        if (!whole)
+#pragma unroll
+            for (int u = 0; u < U; ++u) correct_unit(x, (c0 + u * kTurn) / 8 + lane, end, v[u], -__builtin_inff());
+#pragma unroll
+        for (int u = 0; u < U; ++u) top[u] = add(st, v[u]);
         if constexpr (TOP) {
             // A bound at turns 0, 1, 3, 7, ...: it rises with the logarithm of what was seen.  The lanes' largest columns are columns of their own: the k-th largest
             // among those of all waves is reached by k of the row.  A wave may read what the others saw some turns ago: that is a bound too.

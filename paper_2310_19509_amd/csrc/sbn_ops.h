@@ -101,14 +101,19 @@ __device__ inline Raw<T> fetch_unit(const T* row, long long unit, long long cols
     return cols >= 8 ? fetch<ONCE>(row + min(unit * 8, cols - 8)) : Raw<T>{};
 }
 template <class T>
-__device__ inline void expand_unit(const Raw<T>& r, const T* row, long long unit, long long cols, float (&v)[8], float rest)
+__device__ inline void correct_unit(const T* row, long long unit, long long cols, float (&v)[8], float rest)
 {
-    expand(r, v);
     const long long left = cols - unit * 8;
     if (left < 8) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = i < left ? Elem<T>::get(row[unit * 8 + i]) : rest;
     }
+}
+template <class T>
+__device__ inline void expand_unit(const Raw<T>& r, const T* row, long long unit, long long cols, float (&v)[8], float rest)
+{
+    expand(r, v);
+    correct_unit(row, unit, cols, v, rest);
 }
 __device__ inline void store8(float* p, const float (&v)[8])
 {
