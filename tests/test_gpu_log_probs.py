@@ -47,8 +47,8 @@ def _close(got, want, tol):
     assert np.all(off <= np.broadcast_to(tol, want.shape)[both]), float((off / np.broadcast_to(tol, want.shape)[both]).max())
 
 
-def _compare(x, t, k):
-    got = _score(x, t, k)
+def _compare(x, t, k, got=None):
+    got = got or _score(x, t, k)
     x64 = x.double().cpu().numpy()
     want = L.log_probs(x64, np.zeros((x.shape[0], 0), dtype=np.int64) if t is None else t.cpu().numpy(), k)
     # e^d in 32 bits: its argument is rounded twice (2^-23 of |d|, which its weight e^d keeps below 1 in every sum), its value a few times: 2^-21 of a sum
@@ -80,6 +80,24 @@ def test_many_rows(dtype, rows, cols, pad, n, k, masked):
     x[11] = torch.arange(cols, device="cuda") * 0.01
     x[13] = 2.0
     _compare(x, _targets(cols, rows, cols, n), k)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("cols,pad,k,masked", [(16384, 0, 0, 0.0), (20003, 1, 0, 0.4), (28671, 0, 0, 0.0), (16391, 2, 5, 0.1)])
+def test_many_long_rows(dtype, cols, pad, k, masked):
+    """Twelve rows over and over: the same bits wherever they lie, and those of 64 bits."""
+    base, few = _logits(cols, 12, cols, dtype, 0, masked), _targets(cols, 12, cols, 2)
+    base[7] = -INF
+    base[9, cols // 2] = float("nan")
+    base[10, cols - 1] = INF
+    base[11] = torch.arange(cols, device="cuda") * 0.001
+    pick = torch.arange(2050, device="cuda") % 12
+    x = torch.empty(2050, cols + pad, dtype=dtype, device="cuda")[:, :cols]
+    x.copy_(base[pick])
+    got = _score(x, few[pick], k)
+    for v in got:
+        assert np.array_equal(v, v[:12][pick.cpu().numpy()], equal_nan=v.dtype != np.int64)
+    _compare(base, few, k, [v[:12] for v in got])
 
 
 @pytest.mark.parametrize("cols", [100, 5000, 40000])
