@@ -280,7 +280,7 @@ __device__ inline int join_lists(Key (*lists)[kHold], int* counts, int n, int k)
 }
 
 // One slice of a row to a workgroup, whose waves take steps of 512 columns in turn, so that each sees ascending columns; SOLO: a row to a wave.
-// 2048 x 50001 in 32 bits, four given columns, five alternatives: 410 MB in 79.5 us, 5.2 TB/s; 4096 x 32768 in bfloat16 without alternatives 58 us, 4.6 TB/s;
+// 2048 x 50001 in 32 bits, four given columns, five alternatives: 410 MB in 78.2 us, 5.2 TB/s; 4096 x 32768 in bfloat16 without alternatives 54 us, 5.0 TB/s;
 // one row of 131072, twenty alternatives, 7 us and 7 for the join, of which the reads are a fraction.
 template <class T, bool TOP, bool SOLO, bool ONCE>
 __global__ __launch_bounds__(64 * kWaves, TOP ? 4 : 1) void score_kernel(const T* __restrict__ logits, const Args a)
