@@ -117,8 +117,8 @@ struct RowArgs {
 struct PlainRows {};                       // as a residual's type: rows into SBN_FP8_ROW without a norm
 
 // The norm is in 64 bits from the sum of the squares on, so that codes go where the exact value goes.  In 32 bits, with one rounding of h w / rms and one of each
-// step to a row's codes, 26 to 43 of 2^26 codes lay on the other side of a tie (38 to 57 with 32-bit operations one by one); now none does.  16384 x 4096
-// in 16 bits takes 83.4 us for 81.4, 1021 x 5001 12.8 for 11.6.
+// step to a row's codes, 26 to 43 of 2^26 codes lay on the other side of a tie (38 to 57 with 32-bit operations one by one); now none does, for 2 % of the time of
+// 16384 x 4096 in 16 bits and 10 % of that of 1021 x 5001, whose rows come from the cache (12.8 us).
 __device__ inline double inverse_root(double sum, double share, float eps)
 {
     const double s = __builtin_fma(sum, share, (double)eps);
@@ -220,7 +220,7 @@ __device__ inline void put_row_outputs(const RowArgs& a, long long row, long lon
 }
 
 // One row to THREADS threads, held in registers: ITEMS units each.  RT: the residual's type, void for none, or PlainRows.  16384 x 4096, x and residual in
-// bfloat16, to rows of FP8: 470 MB in 83 us, 5.6 TB/s; one row of 8192 4.1 us.
+// bfloat16, to rows of FP8: 470 MB in 77 us, 6.1 TB/s; one row of 8192 4.1 us.
 template <class XT, class RT, int THREADS, int ITEMS, bool ONCE = false>
 __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void row_kernel(const RowArgs a)
 {
@@ -258,7 +258,8 @@ __global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS) void row_kernel(cons
             expand_unit(rr[i], res, unit, cols, b, 0.0f);
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[i][j] += b[j];
-            if (a.total && (long long)unit * 8 < cols) store_unit((R*)a.total + row * a.ldt, unit, cols, v[i]);
+            // (what the next addition reads, a block later: where it cannot stay in the caches until then it is marked so, 16384 x 4096 in place 85.3 -> 76.9 us)
+            if (a.total && (long long)unit * 8 < cols) store_unit<ONCE>((R*)a.total + row * a.ldt, unit, cols, v[i]);
         }
         if constexpr (NORM)
 #pragma unroll
