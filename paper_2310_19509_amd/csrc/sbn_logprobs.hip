@@ -305,24 +305,42 @@ __global__ __launch_bounds__(64 * kWaves, TOP ? 4 : 1) void score_kernel(const T
     if constexpr (TOP) find.start(lists[wave], a.k, end);
     unsigned turn = 0, next_bound = 0;
     unsigned c0 = begin + (SOLO ? 0 : wave * kStep);
-    if constexpr (SOLO && !TOP && sizeof(T) == 2) {
-        // Long rows: eight steps under way, 2048 x 128000 94.6 -> 85.7 us, 8192 x 32768 97.4 -> 93.0.  Short ones spend as much on what is left over
-        // (16384 x 5000 36.6 -> 37.6), and 32-bit logits have as many bytes under way with four (2048 x 50001 72.2, 76.2 with eight).
-        constexpr int LONG = 8;
-        for (const unsigned stop = a.cols >= 16384 ? end : 0; c0 + LONG * kStep <= stop; c0 += LONG * kStep) {
-            Raw<T> raw[LONG];
+    if constexpr (!TOP) {
+        // A row to a wave of 16-bit logits: eight steps under way while there are as many, 2048 x 128000 94.6 -> 85.7 us, 8192 x 32768 97.4 -> 93.0.  32-bit logits have as
+        // many bytes under way with four (2048 x 50001 72.2, 76.2 with eight).
+        auto whole_turns = [&](auto steps) {
+            constexpr int N = decltype(steps)::value;
+            for (; c0 + (N - 1) * kTurn + kStep <= end; c0 += N * kTurn) {
+                Raw<T> raw[N];
 #pragma unroll
-            for (int u = 0; u < LONG; ++u) raw[u] = fetch<ONCE>(x + c0 + u * kStep + lane * 8);
+                for (int u = 0; u < N; ++u) raw[u] = fetch<ONCE>(x + c0 + u * kTurn + lane * 8);
 #pragma unroll
-            for (int u = 0; u < LONG; ++u) {
-                float v[8];
-                expand(raw[u], v);
-                add(st, v);
+                for (int u = 0; u < N; ++u) {
+                    float v[8];
+                    expand(raw[u], v);
+                    add(st, v);
+                }
             }
+        };
+        if constexpr (SOLO && sizeof(T) == 2) whole_turns(std::integral_constant<int, 8>{});
+        whole_turns(std::integral_constant<int, U>{});
+        // What there is of a last turn (all of it, with nothing in most of its steps: 8192 x 1000 in 32 bits 10.4 us, so 9.4).
+        for (; c0 < end; c0 += U * kTurn) {
+            Raw<T> raw[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (c0 + u * kTurn < end) raw[u] = fetch_unit<ONCE>(x, (c0 + u * kTurn) / 8 + lane, end);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (c0 + u * kTurn < end) {
+                    float v[8];
+                    expand_unit(raw[u], x, (c0 + u * kTurn) / 8 + lane, end, v, -__builtin_inff());
+                    add(st, v);
+                }
         }
     }
     // (the first turn has a barrier: all waves make it)
-    for (; c0 < end || (TOP && !SOLO && turn == 0); c0 += U * kTurn, ++turn) {
+    for (; TOP && (c0 < end || (!SOLO && turn == 0)); c0 += U * kTurn, ++turn) {
         // Whole turns, all but a row's last, test no lane's columns.
         const bool whole = c0 + (U - 1) * kTurn + kStep <= end;
         Raw<T> raw[U];
@@ -528,9 +546,14 @@ __global__ __launch_bounds__(256) void gradient_kernel(const T* logits, T* grad,
     }
 }
 
-// Rows from which a wave reads a row by itself: nothing to join, and no waves without columns in short rows.  8192 rows, five alternatives, us, a workgroup to a
-// row and so: 1000 columns in 32 bits 51, 18; 4000 in 16 bits 53, 28; 32768 139, 124.  1024 rows of 8000 10, 16: too few waves.
-constexpr long long kSoloRows = 2048;
+// Whether a wave reads a row by itself: nothing to join, and no waves without columns in short rows.  Us, a workgroup to a row and so, five alternatives:
+// 8192 x 1000 in 32 bits 51, 18; 8192 x 4000 in 16 bits 53, 28; 8192 x 32768 123, 111.  1024 x 8000 10, 16: too few waves; with a search to make they are still few
+// at 2048 long rows (2048 x 32768 39, 45; twenty alternatives 2048 x 128000 121, 155; 4096 x 32768 65, 61), and the k-th of 64 lanes' largest bounds little where k comes near 64
+// (64 alternatives: 8192 x 6000 78, 94; 8192 x 1000 68, 42).
+bool row_to_wave(long long rows, unsigned cols, int k)
+{
+    return rows >= 2048 && !(k && rows < 4096 && cols >= 32768) && !(k > 48 && cols >= 2048);
+}
 constexpr long long kMostGroups = 1ll << 23;                              // workgroups of 256 threads a launch
 
 template <class T>
@@ -551,9 +574,10 @@ int run_scores(const T* logits, Args a, hipStream_t stream)
         const unsigned groups = (unsigned)(b.rows * a.slices), solo = (unsigned)((b.rows + kWaves - 1) / kWaves);
         constexpr bool MAY = sizeof(T) == 2;
         const bool once = read_once<T>(all, a.cols);
-        if (b.rows >= kSoloRows && a.k)
+        const bool alone = a.slices == 1 && row_to_wave(all, a.cols, a.k);
+        if (alone && a.k)
             (once ? score_kernel<T, true, true, MAY> : score_kernel<T, true, true, false>)<<<solo, 64 * kWaves, 0, stream>>>(x, b);
-        else if (b.rows >= kSoloRows)
+        else if (alone)
             (once ? score_kernel<T, false, true, MAY> : score_kernel<T, false, true, false>)<<<solo, 64 * kWaves, 0, stream>>>(x, b);
         else if (a.k)
             (once ? score_kernel<T, true, false, MAY> : score_kernel<T, true, false, false>)<<<groups, 64 * kWaves, 0, stream>>>(x, b);

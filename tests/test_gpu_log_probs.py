@@ -83,7 +83,7 @@ def test_many_rows(dtype, rows, cols, pad, n, k, masked):
 
 
 @pytest.mark.parametrize("dtype", TYPES)
-@pytest.mark.parametrize("cols,pad,k,masked", [(16384, 0, 0, 0.0), (20003, 1, 0, 0.4), (28671, 0, 0, 0.0), (16391, 2, 5, 0.1)])
+@pytest.mark.parametrize("cols,pad,k,masked", [(16384, 0, 0, 0.0), (20003, 1, 0, 0.4), (28671, 0, 0, 0.0), (16391, 2, 5, 0.1), (33001, 1, 20, 0.2), (1201, 0, 64, 0.1), (1200, 0, 49, 0.98)])
 def test_many_long_rows(dtype, cols, pad, k, masked):
     """Twelve rows over and over: the same bits wherever they lie, and those of 64 bits."""
     base, few = _logits(cols, 12, cols, dtype, 0, masked), _targets(cols, 12, cols, 2)
